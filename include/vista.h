@@ -319,6 +319,69 @@ vista_status vista_qla_backward(const vista_summarize_desc* desc,
                                 void* workspace, size_t workspace_bytes,
                                 void* hip_stream);
 
+/* ------------------------------------------------ gradients of softmax attention */
+
+/*
+ * Backward of vista_summarize with VISTA_ATTN_SOFTMAX.  The probabilities are formed again from the same inputs: nothing of
+ * the forward call is kept or needed.  Per user and head, with K = X W_k, V = X W_v, P = RowSoftmax(scale Q K^T) and dO = d_out:
+ *     dP = dO V^T,   delta_i = sum_j P_ij dP_ij,   dS = P (dP - delta)
+ *     dV = P^T dO,   dQ = scale dS K,   dK = scale dS^T Q
+ * As in vista_qla_backward the gradients are with respect to the projected keys and values (dX = dK W_k^T + dV W_v^T and
+ * dW_k = X^T dK, dW_v = X^T dV are plain matrix products outside this path).  With VISTA_FLAG_SELF_TERM row i also holds its own
+ * key k' = q W_k and value v' = q W_v, which are values of their own here: with p' and ds' = p' (dO . v' - delta) of that column
+ *     dV' = p' dO,   dK' = scale ds' q,   dQ += scale ds' k'
+ *
+ *   desc            as for the forward call; attn = VISTA_ATTN_SOFTMAX, any other form is VISTA_ERR_UNSUPPORTED
+ *   d_out           device [B, S, d]  dtype   gradient of the loss w.r.t. the forward output
+ *   d_queries       device [B, S, d]  dtype   per user, also when the queries are shared (the gradient of shared seeds is
+ *                                             the sum over users); zeros for users without history
+ *   d_keys, d_values device [N, d]    dtype   every row is written
+ *   d_self_keys, d_self_values  device [B, S, d]  dtype   with VISTA_FLAG_SELF_TERM only (else ignored, may be NULL): per user,
+ *                   zeros for users without history
+ *   workspace       >= vista_summarize_backward_workspace_bytes(desc), 256-byte aligned; status word as in vista_summarize.
+ *                   It holds nothing between calls; calls that may overlap in time need one each.
+ * No output overlaps an input or another output.  Equal calls give equal bits.
+ * Supported: every shape and dtype vista_summarize takes; tensors aligned to their elements.
+ */
+size_t vista_summarize_backward_workspace_bytes(const vista_summarize_desc* desc);
+vista_status vista_summarize_backward(const vista_summarize_desc* desc,
+                                      const void* history_emb,
+                                      const int64_t* offsets,
+                                      const int64_t* offsets_host,
+                                      const void* virtual_queries,
+                                      const void* W_k,
+                                      const void* W_v,
+                                      const void* d_out,
+                                      void* d_queries,
+                                      void* d_keys,
+                                      void* d_values,
+                                      void* d_self_keys,
+                                      void* d_self_values,
+                                      void* workspace, size_t workspace_bytes,
+                                      void* hip_stream);
+
+/*
+ * Backward of vista_target_attend (same descriptor).  Per user and head, Y = summaries (keys and values at once):
+ *     P = RowSoftmax(scale Q Y^T),   dP = dO Y^T,   dS = P (dP - rowsum(P dP))
+ *     d_candidates = scale dS Y,     d_summaries = scale dS^T Q + P^T dO
+ * With VISTA_FLAG_SELF_TERM a candidate q is one more key and value of its own row (score scale |q|^2), and that part is
+ * in its gradient:  d_candidates += 2 scale ds' q + p' dO.
+ *
+ *   d_out, d_candidates  device [B, C, d] dtype     d_summaries  device [B, S, d] dtype
+ *   workspace            >= vista_target_attend_backward_workspace_bytes(desc), 256-byte aligned; nothing is kept in it
+ * No output overlaps an input or another output.  Equal calls give equal bits.
+ * Supported: every shape and dtype vista_target_attend takes; tensors aligned to their elements.
+ */
+size_t vista_target_attend_backward_workspace_bytes(const vista_attend_desc* desc);
+vista_status vista_target_attend_backward(const vista_attend_desc* desc,
+                                          const void* candidates,
+                                          const void* summaries,
+                                          const void* d_out,
+                                          void* d_candidates,
+                                          void* d_summaries,
+                                          void* workspace, size_t workspace_bytes,
+                                          void* hip_stream);
+
 /* ------------------------------------------------ cache codec (int8) */
 
 /*
@@ -401,6 +464,48 @@ vista_status vista_sglu_ffn(const vista_ffn_desc* desc,
                             const void* W_g, const void* W_u, const void* W_o,
                             void* out,
                             void* hip_stream);
+
+/* ------------------------------------------------ layer norm */
+
+typedef struct {
+  int64_t rows;   /* items, summaries or candidates; 0 is allowed */
+  int32_t d;      /* width, 1..1024                 */
+  int32_t dtype;  /* VISTA_F32 or VISTA_BF16        */
+  float   eps;    /* 0 selects 1e-6                 */
+} vista_norm_desc;
+
+/*
+ * Layer norm of rows: of item embeddings on their way into a layer, of summaries between two.
+ *     z = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps),   y = z * weight + bias
+ *   x, y          device [rows, d]  dtype; y may be x itself
+ *   weight, bias  device [d]        dtype, each may be NULL (1 and 0)
+ * Mean, deviations and y are formed in fp32.  A row that is not finite stays so by itself.  No workspace.
+ */
+vista_status vista_layer_norm(const vista_norm_desc* desc,
+                              const void* x,
+                              const void* weight, const void* bias,
+                              void* y,
+                              void* hip_stream);
+
+/*
+ * Its gradients, z formed again from x:  with g = d_y * weight,
+ *     d_x = (g - mean(g) - z mean(g z)) / sqrt(mean((x - mean(x))^2) + eps)
+ *     d_weight = sum over rows of d_y z,   d_bias = sum over rows of d_y
+ *   d_y, d_x          device [rows, d]  dtype; d_x may be d_y itself
+ *   d_weight, d_bias  device [d]        dtype, each may be NULL where it is not wanted; zeros for rows = 0
+ *   workspace         >= vista_layer_norm_backward_workspace_bytes(desc), 256-byte aligned; nothing is kept in it.
+ *                     Not read, and may be NULL, where d_weight and d_bias are.
+ * Sums over rows are fp32 and in a fixed order: equal calls give equal bits.
+ */
+size_t vista_layer_norm_backward_workspace_bytes(const vista_norm_desc* desc);
+vista_status vista_layer_norm_backward(const vista_norm_desc* desc,
+                                       const void* x,
+                                       const void* weight,
+                                       const void* d_y,
+                                       void* d_x,
+                                       void* d_weight, void* d_bias,
+                                       void* workspace, size_t workspace_bytes,
+                                       void* hip_stream);
 
 /* Static, human-readable name of a status code. */
 const char* vista_status_string(int status);

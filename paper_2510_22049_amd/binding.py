@@ -39,6 +39,13 @@ EXPORTS = (
     "vista_summarize_q8",
     "vista_qla_backward_workspace_bytes",
     "vista_qla_backward",
+    "vista_summarize_backward_workspace_bytes",
+    "vista_summarize_backward",
+    "vista_target_attend_backward_workspace_bytes",
+    "vista_target_attend_backward",
+    "vista_layer_norm",
+    "vista_layer_norm_backward_workspace_bytes",
+    "vista_layer_norm_backward",
     "vista_sglu_ffn",
 )
 
@@ -62,6 +69,10 @@ class CodecDesc(C.Structure):
 class FfnDesc(C.Structure):
     _fields_ = [("rows", C.c_int64), ("d", C.c_int32), ("d_ff", C.c_int32),
                 ("dtype", C.c_int32), ("eps", C.c_float)]
+
+
+class NormDesc(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("d", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float)]
 
 
 class VistaError(RuntimeError):
@@ -104,6 +115,20 @@ def lib() -> C.CDLL:
     L.vista_qla_backward_workspace_bytes.argtypes = [C.POINTER(SummarizeDesc)]
     L.vista_qla_backward.restype = C.c_int
     L.vista_qla_backward.argtypes = [C.POINTER(SummarizeDesc)] + [vp] * 13 + [C.c_size_t, vp]
+    L.vista_summarize_backward_workspace_bytes.restype = C.c_size_t
+    L.vista_summarize_backward_workspace_bytes.argtypes = [C.POINTER(SummarizeDesc)]
+    L.vista_summarize_backward.restype = C.c_int
+    L.vista_summarize_backward.argtypes = [C.POINTER(SummarizeDesc)] + [vp] * 13 + [C.c_size_t, vp]
+    L.vista_target_attend_backward_workspace_bytes.restype = C.c_size_t
+    L.vista_target_attend_backward_workspace_bytes.argtypes = [C.POINTER(AttendDesc)]
+    L.vista_target_attend_backward.restype = C.c_int
+    L.vista_target_attend_backward.argtypes = [C.POINTER(AttendDesc)] + [vp] * 6 + [C.c_size_t, vp]
+    L.vista_layer_norm.restype = C.c_int
+    L.vista_layer_norm.argtypes = [C.POINTER(NormDesc)] + [vp] * 5
+    L.vista_layer_norm_backward_workspace_bytes.restype = C.c_size_t
+    L.vista_layer_norm_backward_workspace_bytes.argtypes = [C.POINTER(NormDesc)]
+    L.vista_layer_norm_backward.restype = C.c_int
+    L.vista_layer_norm_backward.argtypes = [C.POINTER(NormDesc)] + [vp] * 7 + [C.c_size_t, vp]
     L.vista_quantize_summaries.restype = C.c_int
     L.vista_quantize_summaries.argtypes = [C.POINTER(CodecDesc), vp, vp, vp, vp]
     L.vista_target_attend_q8.restype = C.c_int
@@ -130,6 +155,35 @@ def _dev(t: torch.Tensor, name: str) -> int:
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
+
+
+def _shaped(like: torch.Tensor, **tensors) -> None:
+    """Each tensor has the shape it is given with, the type of `like` and its device, which is the current one (the call
+    goes to the current device's stream): a kernel would otherwise read or write past the end of one of them."""
+    if like.is_cuda and like.device.index != torch.cuda.current_device():
+        raise ValueError("the tensors live on another device than the current one")
+    for name, (t, shape) in tensors.items():
+        if t is None:
+            continue
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+        if t.dtype != like.dtype:
+            raise TypeError(f"{name} must be {like.dtype}, not {t.dtype}")
+        if t.device != like.device:
+            raise ValueError(f"{name} must live on {like.device}")
+
+
+def _workspace(workspace, need, like: torch.Tensor) -> torch.Tensor:
+    """The caller's workspace, or one of torch's of need() bytes where there is none."""
+    if workspace is None:
+        return torch.empty(max(need(), 256), dtype=torch.uint8, device=like.device)
+    if workspace.dtype != torch.uint8 or workspace.device != like.device:
+        raise ValueError(f"workspace must be uint8 on {like.device}")
+    return workspace
+
+
+def _optional(t, name: str):
+    return None if t is None else _dev(t, name)
 
 
 def _stream_getter():
@@ -260,6 +314,71 @@ def vista_qla_backward(history_emb, offsets, virtual_queries, W_k, W_v, d_out, d
     return workspace
 
 
+def vista_summarize_backward(history_emb, offsets, virtual_queries, W_k, W_v, d_out, d_queries, d_keys, d_values, *, H,
+                             scale=0.0, segment_items=0, offsets_host=None, workspace=None, d_self_keys=None,
+                             d_self_values=None):
+    """Gradients of softmax summarization: d_out [B,S,d] -> d_queries [B,S,d], d_keys / d_values [N,d] (of the projected
+    keys and values); with d_self_keys and d_self_values [B,S,d] given, the forward had the self term and its gradients
+    are formed as well.  Returns the workspace, which may be passed to the next call."""
+    if offsets.dtype != torch.int64 or offsets.dim() != 1 or offsets.numel() < 2:
+        raise TypeError("offsets must be int64 [B + 1]")
+    if offsets.device != history_emb.device:
+        raise ValueError("offsets must live where history_emb does")
+    if virtual_queries.dim() not in (2, 3) or history_emb.dim() != 2:
+        raise ValueError("history_emb must be [N, d] and virtual_queries [S, d] or [B, S, d]")
+    B = offsets.numel() - 1
+    S, d = virtual_queries.shape[-2:]
+    N = history_emb.shape[0]
+    per_user = virtual_queries.dim() == 3
+    if (d_self_keys is None) != (d_self_values is None):
+        raise ValueError("d_self_keys and d_self_values go together")
+    _shaped(history_emb, history_emb=(history_emb, (N, d)), virtual_queries=(virtual_queries, (B, S, d) if per_user else (S, d)),
+            W_k=(W_k, (d, d)), W_v=(W_v, (d, d)), d_out=(d_out, (B, S, d)), d_queries=(d_queries, (B, S, d)),
+            d_keys=(d_keys, (N, d)), d_values=(d_values, (N, d)), d_self_keys=(d_self_keys, (B, S, d)),
+            d_self_values=(d_self_values, (B, S, d)))
+    desc = summarize_desc(B, S, d, H, _dtype_code(history_emb), N, per_user, scale, segment_items, VISTA_ATTN_SOFTMAX,
+                          d_self_keys is not None)
+    host = None
+    if offsets_host is not None:
+        if offsets_host.is_cuda or offsets_host.dtype != torch.int64 or offsets_host.numel() != B + 1:
+            raise ValueError("offsets_host must be a CPU int64 tensor of B + 1 entries")
+        offsets_host = offsets_host.contiguous()
+        host = offsets_host.data_ptr()
+    workspace = _workspace(workspace, lambda: lib().vista_summarize_backward_workspace_bytes(C.byref(desc)), history_emb)
+    rows = (lambda t, name: _dev(t, name)) if N else (lambda t, name: None)
+    st = lib().vista_summarize_backward(C.byref(desc), rows(history_emb, "history_emb"), _dev(offsets, "offsets"), host,
+                                        _dev(virtual_queries, "virtual_queries"), _dev(W_k, "W_k"), _dev(W_v, "W_v"),
+                                        _dev(d_out, "d_out"), _dev(d_queries, "d_queries"), rows(d_keys, "d_keys"),
+                                        rows(d_values, "d_values"), _optional(d_self_keys, "d_self_keys"),
+                                        _optional(d_self_values, "d_self_values"), _dev(workspace, "workspace"),
+                                        workspace.numel(), _stream())
+    if st != VISTA_OK:
+        raise VistaError(st)
+    return workspace
+
+
+def vista_target_attend_backward(candidates, summaries, d_out, d_candidates, d_summaries, *, H, scale=0.0, self_term=False,
+                                 workspace=None):
+    """Gradients of candidate attention: d_out [B,C,d] -> d_candidates [B,C,d], d_summaries [B,S,d].  Returns the
+    workspace, which may be passed to the next call."""
+    if candidates.dim() != 3 or summaries.dim() != 3:
+        raise ValueError("candidates must be [B, C, d] and summaries [B, S, d]")
+    B, Cn, d = candidates.shape
+    S = summaries.shape[1]
+    _shaped(candidates, candidates=(candidates, (B, Cn, d)), summaries=(summaries, (B, S, d)), d_out=(d_out, (B, Cn, d)),
+            d_candidates=(d_candidates, (B, Cn, d)), d_summaries=(d_summaries, (B, S, d)))
+    desc = AttendDesc(B=B, C=Cn, S=S, d=d, H=H, dtype=_dtype_code(candidates), scale=scale,
+                      flags=VISTA_FLAG_SELF_TERM if self_term else 0)
+    workspace = _workspace(workspace, lambda: lib().vista_target_attend_backward_workspace_bytes(C.byref(desc)), candidates)
+    st = lib().vista_target_attend_backward(C.byref(desc), _dev(candidates, "candidates"), _dev(summaries, "summaries"),
+                                            _dev(d_out, "d_out"), _dev(d_candidates, "d_candidates"),
+                                            _dev(d_summaries, "d_summaries"), _dev(workspace, "workspace"),
+                                            workspace.numel(), _stream())
+    if st != VISTA_OK:
+        raise VistaError(st)
+    return workspace
+
+
 def vista_quantize_summaries(y, codes, scales, *, H):
     """Cache codec: y [..., d] -> codes int8 [..., d], scales float32 [..., H] (device tensors)."""
     d = y.shape[-1]
@@ -329,3 +448,37 @@ def vista_sglu_ffn(y, W_g, W_u, W_o, out, *, eps=0.0):
                               _dev(W_o, "W_o"), _dev(out, "out"), _stream())
     if st != VISTA_OK:
         raise VistaError(st)
+
+
+def _norm_rows(x: torch.Tensor) -> NormDesc:
+    d = x.shape[-1]
+    return NormDesc(rows=x.numel() // d if d else 0, d=d, dtype=_dtype_code(x))
+
+
+def vista_layer_norm(x, weight, bias, y, *, eps=0.0):
+    """Layer norm of the rows of x [..., d] into y (which may be x); weight and bias [d], each may be None."""
+    desc = _norm_rows(x)
+    desc.eps = eps
+    _shaped(x, weight=(weight, (desc.d,)), bias=(bias, (desc.d,)), y=(y, x.shape))
+    st = lib().vista_layer_norm(C.byref(desc), _dev(x, "x"), _optional(weight, "weight"), _optional(bias, "bias"), _dev(y, "y"),
+                                _stream())
+    if st != VISTA_OK:
+        raise VistaError(st)
+
+
+def vista_layer_norm_backward(x, weight, d_y, d_x, d_weight, d_bias, *, eps=0.0, workspace=None):
+    """Gradients of layer norm: d_y [..., d] -> d_x (which may be d_y), d_weight and d_bias [d] (each may be None).  Returns
+    the workspace, which may be passed to the next call; None where neither sum is wanted."""
+    desc = _norm_rows(x)
+    desc.eps = eps
+    _shaped(x, weight=(weight, (desc.d,)), d_y=(d_y, x.shape), d_x=(d_x, x.shape), d_weight=(d_weight, (desc.d,)),
+            d_bias=(d_bias, (desc.d,)))
+    if d_weight is not None or d_bias is not None:
+        workspace = _workspace(workspace, lambda: lib().vista_layer_norm_backward_workspace_bytes(C.byref(desc)), x)
+    st = lib().vista_layer_norm_backward(C.byref(desc), _dev(x, "x"), _optional(weight, "weight"), _dev(d_y, "d_y"),
+                                         _dev(d_x, "d_x"), _optional(d_weight, "d_weight"), _optional(d_bias, "d_bias"),
+                                         _optional(workspace, "workspace"), workspace.numel() if workspace is not None else 0,
+                                         _stream())
+    if st != VISTA_OK:
+        raise VistaError(st)
+    return workspace

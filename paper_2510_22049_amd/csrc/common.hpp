@@ -86,6 +86,19 @@ __device__ __forceinline__ int64_t segment_of(int64_t row, int seg) {
   return (uint64_t(row) >> 32) == 0 ? int64_t(uint32_t(row) / uint32_t(seg)) : row / seg;
 }
 
+// The status word, published by a launch's first block: without a plan kernel in front the offsets are
+// checked here, unless the host has done that (N < 0).
+__device__ __forceinline__ void publish_status(const int64_t* __restrict__ offsets, int B, int64_t N, int* status) {
+  int bad = 0;
+  if (N >= 0)
+    for (int u = threadIdx.x; u <= B; u += blockDim.x) {
+      const int64_t v = offsets[u];
+      bad |= (u == 0 && v != 0) || (u == B && v != N) || (u < B && offsets[u + 1] < v);
+    }
+  bad = __syncthreads_or(bad);
+  if (threadIdx.x == 0) *status = bad ? int(VISTA_ERR_OFFSETS) : int(VISTA_OK);
+}
+
 struct Piece {
   int user;
   int64_t begin, end;  // flat rows [begin, end)
@@ -260,6 +273,22 @@ vista_status generic_sglu_ffn(const vista_ffn_desc& d, float eps, const void* y,
 bool mfma_sglu_ffn_supported(const vista_ffn_desc& d);
 vista_status mfma_sglu_ffn(const vista_ffn_desc& d, float eps, const void* y, const void* Wg,
                            const void* Wu, const void* Wo, void* out, hipStream_t s);
+
+// gradients of softmax attention: fp32 matrix instructions (grad_f32.hip)
+int f32_grad_segment(const vista_summarize_desc& d);
+size_t f32_summarize_backward_workspace(const vista_summarize_desc& d);
+vista_status f32_summarize_backward(const SummarizeArgs& a, const void* d_out, void* d_queries, void* d_keys, void* d_values,
+                                    void* d_self_keys, void* d_self_values);
+size_t f32_attend_backward_workspace(const vista_attend_desc& d);
+vista_status f32_attend_backward(const vista_attend_desc& d, float scale, const void* cand, const void* summ, const void* d_out,
+                                 void* d_cand, void* d_summ, void* workspace, hipStream_t s);
+
+// layer norm (norm.hip)
+vista_status layer_norm(const vista_norm_desc& d, float eps, const void* x, const void* w, const void* b, void* y,
+                        hipStream_t s);
+size_t layer_norm_backward_workspace(const vista_norm_desc& d);
+vista_status layer_norm_backward(const vista_norm_desc& d, float eps, const void* x, const void* w, const void* dy, void* dx,
+                                 void* dw, void* db, void* workspace, hipStream_t s);
 
 // Validates offsets on the device (status word) and records, for every segment,
 // the user that owns its first row (seg_user[g], int32), so that the main

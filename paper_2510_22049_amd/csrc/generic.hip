@@ -51,19 +51,6 @@ hipError_t launch_plan(const int64_t* offsets, int B, int64_t N, int seg, int64_
   return launch(plan_kernel, dim3(blocks), dim3(256), 0, s, offsets, B, N, seg, G, status, seg_user);
 }
 
-// The status word, published by a launch's first block: without a plan kernel in front the offsets are
-// checked here, unless the host has done that (N < 0).
-__device__ __forceinline__ void publish_status(const int64_t* __restrict__ offsets, int B, int64_t N, int* status) {
-  int bad = 0;
-  if (N >= 0)
-    for (int u = threadIdx.x; u <= B; u += blockDim.x) {
-      const int64_t v = offsets[u];
-      bad |= (u == 0 && v != 0) || (u == B && v != N) || (u < B && offsets[u + 1] < v);
-    }
-  bad = __syncthreads_or(bad);
-  if (threadIdx.x == 0) *status = bad ? int(VISTA_ERR_OFFSETS) : int(VISTA_OK);
-}
-
 // -------------------------------------------------- stage 1: K/V projection
 // K = X W_k, V = X W_v in fp32 (Sec. 3.2.1: K and V of shape (L, d)).
 // Block = 256 threads = (256/d') rows x d' columns; each thread one (row, col).

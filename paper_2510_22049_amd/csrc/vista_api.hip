@@ -28,6 +28,15 @@ vista_status check_summarize_desc(const vista_summarize_desc* d) {
   return VISTA_OK;
 }
 
+// The host mirror of the offsets, where one is given.
+vista_status check_offsets(const vista_summarize_desc* d, const int64_t* offsets_host) {
+  if (!offsets_host) return VISTA_OK;
+  if (offsets_host[0] != 0 || offsets_host[d->B] != d->total_items) return VISTA_ERR_OFFSETS;
+  for (int b = 0; b < d->B; ++b)
+    if (offsets_host[b + 1] < offsets_host[b]) return VISTA_ERR_OFFSETS;
+  return VISTA_OK;
+}
+
 // Default segment size: a function of N alone (never of the device probed at
 // run time).  The history is cut into 256 k equal segments -- one workgroup per
 // compute unit of the target part and k rounds -- with k the smallest count
@@ -188,11 +197,8 @@ static vista_status summarize_impl(const vista_summarize_desc* desc, const void*
   if (out_scales && !mfma_summarize_supported(*desc)) return VISTA_ERR_UNSUPPORTED;
   if (!offsets || !virtual_queries || !W_k || !W_v || !out) return VISTA_ERR_NULL;
   if (desc->total_items > 0 && !history_emb) return VISTA_ERR_NULL;
-  if (offsets_host) {
-    if (offsets_host[0] != 0 || offsets_host[desc->B] != desc->total_items) return VISTA_ERR_OFFSETS;
-    for (int b = 0; b < desc->B; ++b)
-      if (offsets_host[b + 1] < offsets_host[b]) return VISTA_ERR_OFFSETS;
-  }
+  st = check_offsets(desc, offsets_host);
+  if (st != VISTA_OK) return st;
   // a workspace that holds the base schedule only gets the base schedule
   Work w = best_work(*desc);
   const Work base = base_work(*desc);
@@ -286,11 +292,8 @@ vista_status vista_qla_backward(const vista_summarize_desc* desc, const void* hi
   if (!offsets || !virtual_queries || !W_k || !W_v || !d_out || !d_queries) return VISTA_ERR_NULL;
   if ((desc->flags & VISTA_FLAG_SELF_TERM) && (!d_self_keys || !d_self_values)) return VISTA_ERR_NULL;
   if (desc->total_items > 0 && (!history_emb || !d_keys || !d_values)) return VISTA_ERR_NULL;
-  if (offsets_host) {
-    if (offsets_host[0] != 0 || offsets_host[desc->B] != desc->total_items) return VISTA_ERR_OFFSETS;
-    for (int b = 0; b < desc->B; ++b)
-      if (offsets_host[b + 1] < offsets_host[b]) return VISTA_ERR_OFFSETS;
-  }
+  st = check_offsets(desc, offsets_host);
+  if (st != VISTA_OK) return st;
   // a workspace that holds the base schedule only gets the base schedule
   int32_t seg = best_work(*desc).seg;
   const int32_t base_seg = resolve_segment(desc);
@@ -344,9 +347,51 @@ vista_status vista_summarize_static(const vista_summarize_desc* desc, const void
                          size_t(VISTA_STATIC_SCRATCH_BYTES), hip_stream);
 }
 
-static vista_status target_attend_impl(const vista_attend_desc* desc, const void* candidates,
-                                       const void* summaries, const int8_t* codes, const float* scales, void* out,
-                                       void* hip_stream) {
+// ------------------------------------------------ gradients of softmax attention
+
+size_t vista_summarize_backward_workspace_bytes(const vista_summarize_desc* desc) {
+  if (check_summarize_desc(desc) != VISTA_OK || desc->attn != VISTA_ATTN_SOFTMAX) return 0;
+  return f32_summarize_backward_workspace(*desc);
+}
+
+vista_status vista_summarize_backward(const vista_summarize_desc* desc, const void* history_emb, const int64_t* offsets,
+                                      const int64_t* offsets_host, const void* virtual_queries, const void* W_k,
+                                      const void* W_v, const void* d_out, void* d_queries, void* d_keys, void* d_values,
+                                      void* d_self_keys, void* d_self_values, void* workspace, size_t workspace_bytes,
+                                      void* hip_stream) {
+  vista_status st = check_summarize_desc(desc);
+  if (st != VISTA_OK) return st;
+  if (desc->attn != VISTA_ATTN_SOFTMAX) return VISTA_ERR_UNSUPPORTED;
+  if (!offsets || !virtual_queries || !W_k || !W_v || !d_out || !d_queries) return VISTA_ERR_NULL;
+  if ((desc->flags & VISTA_FLAG_SELF_TERM) && (!d_self_keys || !d_self_values)) return VISTA_ERR_NULL;
+  if (desc->total_items > 0 && (!history_emb || !d_keys || !d_values)) return VISTA_ERR_NULL;
+  st = check_offsets(desc, offsets_host);
+  if (st != VISTA_OK) return st;
+  SummarizeArgs a;
+  a.desc = *desc;
+  a.seg = f32_grad_segment(*desc);
+  a.G = (desc->total_items + a.seg - 1) / a.seg;
+  if (a.G + desc->B > 0x7FFFFFFF) return VISTA_ERR_UNSUPPORTED;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 ||
+      workspace_bytes < f32_summarize_backward_workspace(*desc))
+    return VISTA_ERR_WORKSPACE;
+  a.seg_user = nullptr;
+  a.offsets_checked = offsets_host != nullptr;
+  a.scale_plain = desc->scale > 0.f ? desc->scale : 1.f / sqrtf(float(desc->d / desc->H));
+  a.scale_log2 = a.scale_plain * kLog2e;
+  a.X = history_emb;
+  a.offsets = offsets;
+  a.Q = virtual_queries;
+  a.Wk = W_k;
+  a.Wv = W_v;
+  a.out = nullptr;
+  a.out_scales = nullptr;
+  a.workspace = static_cast<char*>(workspace);
+  a.stream = static_cast<hipStream_t>(hip_stream);
+  return f32_summarize_backward(a, d_out, d_queries, d_keys, d_values, d_self_keys, d_self_values);
+}
+
+static vista_status check_attend_desc(const vista_attend_desc* desc) {
   if (!desc) return VISTA_ERR_NULL;
   if (desc->B <= 0 || desc->C <= 0 || desc->S <= 0 || desc->d <= 0 || desc->H <= 0) return VISTA_ERR_SHAPE;
   if (desc->d % desc->H != 0) return VISTA_ERR_SHAPE;
@@ -354,6 +399,32 @@ static vista_status target_attend_impl(const vista_attend_desc* desc, const void
   if ((desc->flags & ~VISTA_FLAG_SELF_TERM) != 0) return VISTA_ERR_SHAPE;
   if (!dtype_ok(desc->dtype)) return VISTA_ERR_UNSUPPORTED;
   if (desc->S > 512 || desc->d / desc->H > 64) return VISTA_ERR_UNSUPPORTED;
+  return VISTA_OK;
+}
+
+size_t vista_target_attend_backward_workspace_bytes(const vista_attend_desc* desc) {
+  if (check_attend_desc(desc) != VISTA_OK) return 0;
+  return f32_attend_backward_workspace(*desc);
+}
+
+vista_status vista_target_attend_backward(const vista_attend_desc* desc, const void* candidates, const void* summaries,
+                                          const void* d_out, void* d_candidates, void* d_summaries, void* workspace,
+                                          size_t workspace_bytes, void* hip_stream) {
+  const vista_status st = check_attend_desc(desc);
+  if (st != VISTA_OK) return st;
+  if (!candidates || !summaries || !d_out || !d_candidates || !d_summaries) return VISTA_ERR_NULL;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < f32_attend_backward_workspace(*desc))
+    return VISTA_ERR_WORKSPACE;
+  const float scale = desc->scale > 0.f ? desc->scale : 1.f / sqrtf(float(desc->d / desc->H));
+  return f32_attend_backward(*desc, scale, candidates, summaries, d_out, d_candidates, d_summaries, workspace,
+                             static_cast<hipStream_t>(hip_stream));
+}
+
+static vista_status target_attend_impl(const vista_attend_desc* desc, const void* candidates,
+                                       const void* summaries, const int8_t* codes, const float* scales, void* out,
+                                       void* hip_stream) {
+  const vista_status st = check_attend_desc(desc);
+  if (st != VISTA_OK) return st;
   if (!candidates || !out || (!summaries && !(codes && scales))) return VISTA_ERR_NULL;
   const float scale = desc->scale > 0.f ? desc->scale : 1.f / sqrtf(float(desc->d / desc->H));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
@@ -391,6 +462,40 @@ vista_status vista_sglu_ffn(const vista_ffn_desc* desc, const void* y, const voi
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   if (mfma_sglu_ffn_supported(*desc)) return mfma_sglu_ffn(*desc, eps, y, W_g, W_u, W_o, out, s);
   return generic_sglu_ffn(*desc, eps, y, W_g, W_u, W_o, out, s);
+}
+
+static vista_status check_norm_desc(const vista_norm_desc* desc) {
+  if (!desc) return VISTA_ERR_NULL;
+  if (desc->rows < 0 || desc->d <= 0) return VISTA_ERR_SHAPE;
+  if (!(desc->eps >= 0.f) || isinf(desc->eps)) return VISTA_ERR_SHAPE;
+  if (!dtype_ok(desc->dtype) || desc->d > 1024) return VISTA_ERR_UNSUPPORTED;
+  return VISTA_OK;
+}
+
+vista_status vista_layer_norm(const vista_norm_desc* desc, const void* x, const void* weight, const void* bias, void* y,
+                              void* hip_stream) {
+  const vista_status st = check_norm_desc(desc);
+  if (st != VISTA_OK) return st;
+  if (desc->rows > 0 && (!x || !y)) return VISTA_ERR_NULL;
+  return layer_norm(*desc, desc->eps > 0.f ? desc->eps : 1e-6f, x, weight, bias, y, static_cast<hipStream_t>(hip_stream));
+}
+
+size_t vista_layer_norm_backward_workspace_bytes(const vista_norm_desc* desc) {
+  if (check_norm_desc(desc) != VISTA_OK) return 0;
+  return layer_norm_backward_workspace(*desc);
+}
+
+vista_status vista_layer_norm_backward(const vista_norm_desc* desc, const void* x, const void* weight, const void* d_y,
+                                       void* d_x, void* d_weight, void* d_bias, void* workspace, size_t workspace_bytes,
+                                       void* hip_stream) {
+  const vista_status st = check_norm_desc(desc);
+  if (st != VISTA_OK) return st;
+  if (desc->rows > 0 && (!x || !d_y || !d_x)) return VISTA_ERR_NULL;
+  if ((d_weight || d_bias) && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 ||
+                               workspace_bytes < layer_norm_backward_workspace(*desc)))
+    return VISTA_ERR_WORKSPACE;
+  return layer_norm_backward(*desc, desc->eps > 0.f ? desc->eps : 1e-6f, x, weight, d_y, d_x, d_weight, d_bias, workspace,
+                             static_cast<hipStream_t>(hip_stream));
 }
 
 }  // extern "C"
