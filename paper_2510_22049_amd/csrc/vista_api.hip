@@ -351,7 +351,9 @@ vista_status vista_summarize_static(const vista_summarize_desc* desc, const void
 
 size_t vista_summarize_backward_workspace_bytes(const vista_summarize_desc* desc) {
   if (check_summarize_desc(desc) != VISTA_OK || desc->attn != VISTA_ATTN_SOFTMAX) return 0;
-  return f32_summarize_backward_workspace(*desc);
+  const size_t any = f32_summarize_backward_workspace(*desc);
+  const size_t fast = mfma_summarize_backward_supported(*desc) ? mfma_summarize_backward_workspace(*desc) : 0;
+  return any > fast ? any : fast;        // which of the two a call takes depends on its pointers, too
 }
 
 vista_status vista_summarize_backward(const vista_summarize_desc* desc, const void* history_emb, const int64_t* offsets,
@@ -367,13 +369,18 @@ vista_status vista_summarize_backward(const vista_summarize_desc* desc, const vo
   if (desc->total_items > 0 && (!history_emb || !d_keys || !d_values)) return VISTA_ERR_NULL;
   st = check_offsets(desc, offsets_host);
   if (st != VISTA_OK) return st;
+  // the bf16 kernels move 16 bytes of items, queries and gradients at a time
+  const uintptr_t low = reinterpret_cast<uintptr_t>(history_emb) | reinterpret_cast<uintptr_t>(virtual_queries) |
+                        reinterpret_cast<uintptr_t>(d_out) | reinterpret_cast<uintptr_t>(d_keys) |
+                        reinterpret_cast<uintptr_t>(d_values);
+  const bool fast = mfma_summarize_backward_supported(*desc) && (low & 15) == 0;
   SummarizeArgs a;
   a.desc = *desc;
-  a.seg = f32_grad_segment(*desc);
+  a.seg = fast ? mfma_grad_segment(*desc) : f32_grad_segment(*desc);
   a.G = (desc->total_items + a.seg - 1) / a.seg;
-  if (a.G + desc->B > 0x7FFFFFFF) return VISTA_ERR_UNSUPPORTED;
+  if (a.G + desc->B > 0x7FFFFFFF || (a.G + 8) * desc->H > 0x7FFFFFF) return VISTA_ERR_UNSUPPORTED;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 ||
-      workspace_bytes < f32_summarize_backward_workspace(*desc))
+      workspace_bytes < vista_summarize_backward_workspace_bytes(desc))
     return VISTA_ERR_WORKSPACE;
   a.seg_user = nullptr;
   a.offsets_checked = offsets_host != nullptr;
@@ -388,7 +395,8 @@ vista_status vista_summarize_backward(const vista_summarize_desc* desc, const vo
   a.out_scales = nullptr;
   a.workspace = static_cast<char*>(workspace);
   a.stream = static_cast<hipStream_t>(hip_stream);
-  return f32_summarize_backward(a, d_out, d_queries, d_keys, d_values, d_self_keys, d_self_values);
+  return fast ? mfma_summarize_backward(a, d_out, d_queries, d_keys, d_values, d_self_keys, d_self_values)
+              : f32_summarize_backward(a, d_out, d_queries, d_keys, d_values, d_self_keys, d_self_values);
 }
 
 static vista_status check_attend_desc(const vista_attend_desc* desc) {
