@@ -34,7 +34,8 @@ FLAGS = [
 # Accumulators that the vector unit reads go to ordinary registers: without this a kernel that needs more than 256 registers
 # has every product write the accumulation registers, and each value read costs a move (64 of 293 instructions of the
 # gradients' inner loop).
-SOURCE_FLAGS = {"grad_mfma.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
+_VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
+SOURCE_FLAGS = {"grad_mfma.hip": _VGPR_FORM, "grad_attend_mfma.hip": _VGPR_FORM}
 
 
 def sources():

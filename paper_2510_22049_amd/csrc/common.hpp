@@ -285,6 +285,10 @@ int mfma_grad_segment(const vista_summarize_desc& d);
 size_t mfma_summarize_backward_workspace(const vista_summarize_desc& d);
 vista_status mfma_summarize_backward(const SummarizeArgs& a, const void* d_out, void* d_queries, void* d_keys, void* d_values,
                                      void* d_self_keys, void* d_self_values);
+bool mfma_attend_backward_supported(const vista_attend_desc& d);     // grad_attend_mfma.hip
+size_t mfma_attend_backward_workspace(const vista_attend_desc& d);
+vista_status mfma_attend_backward(const vista_attend_desc& d, float scale, const void* cand, const void* summ, const void* d_out,
+                                  void* d_cand, void* d_summ, void* workspace, hipStream_t s);
 size_t f32_attend_backward_workspace(const vista_attend_desc& d);
 vista_status f32_attend_backward(const vista_attend_desc& d, float scale, const void* cand, const void* summ, const void* d_out,
                                  void* d_cand, void* d_summ, void* workspace, hipStream_t s);

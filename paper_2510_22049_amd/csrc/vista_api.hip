@@ -412,7 +412,9 @@ static vista_status check_attend_desc(const vista_attend_desc* desc) {
 
 size_t vista_target_attend_backward_workspace_bytes(const vista_attend_desc* desc) {
   if (check_attend_desc(desc) != VISTA_OK) return 0;
-  return f32_attend_backward_workspace(*desc);
+  const size_t any = f32_attend_backward_workspace(*desc);
+  const size_t fast = mfma_attend_backward_supported(*desc) ? mfma_attend_backward_workspace(*desc) : 0;
+  return any > fast ? any : fast;
 }
 
 vista_status vista_target_attend_backward(const vista_attend_desc* desc, const void* candidates, const void* summaries,
@@ -421,9 +423,16 @@ vista_status vista_target_attend_backward(const vista_attend_desc* desc, const v
   const vista_status st = check_attend_desc(desc);
   if (st != VISTA_OK) return st;
   if (!candidates || !summaries || !d_out || !d_candidates || !d_summaries) return VISTA_ERR_NULL;
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 || workspace_bytes < f32_attend_backward_workspace(*desc))
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 ||
+      workspace_bytes < vista_target_attend_backward_workspace_bytes(desc))
     return VISTA_ERR_WORKSPACE;
   const float scale = desc->scale > 0.f ? desc->scale : 1.f / sqrtf(float(desc->d / desc->H));
+  const uintptr_t low = reinterpret_cast<uintptr_t>(candidates) | reinterpret_cast<uintptr_t>(summaries) |
+                        reinterpret_cast<uintptr_t>(d_out) | reinterpret_cast<uintptr_t>(d_candidates) |
+                        reinterpret_cast<uintptr_t>(d_summaries);
+  if (mfma_attend_backward_supported(*desc) && (low & 15) == 0)        // they move 16 bytes at a time
+    return mfma_attend_backward(*desc, scale, candidates, summaries, d_out, d_candidates, d_summaries, workspace,
+                                static_cast<hipStream_t>(hip_stream));
   return f32_attend_backward(*desc, scale, candidates, summaries, d_out, d_candidates, d_summaries, workspace,
                              static_cast<hipStream_t>(hip_stream));
 }
