@@ -19,7 +19,8 @@ __device__ __forceinline__ Slots slots_of(const GradRows& r, int64_t b) {
   return {g0 + b, g1 - g0 + 1};
 }
 
-// LPR lanes a row (1 or 64), lane k joins every LPR-th record from its k-th on.
+// LPR lanes a row (8 or 64): lane k joins every LPR-th record from its k-th on, and takes every LPR-th channel of the own key's
+// products.  (One thread a row: 20 us instead of 5 where 9600 rows have a key of their own.)
 template <typename T, int LPR>
 __global__ __launch_bounds__(256) void join_stats_kernel(GradRows r, const float* __restrict__ stats, int rows,
                                                          float* __restrict__ lse, float* __restrict__ delta, const T* Q,
@@ -37,26 +38,26 @@ __global__ __launch_bounds__(256) void join_stats_kernel(GradRows r, const float
       const float* s = stats + (((sl.first + n) * r.H + h) * rows + i) * 3;
       join_stats(m, l, e, s[0], s[1], s[2]);
     }
-    if (LPR > 1) {
-#pragma unroll
-      for (int o = 1; o < LPR; o *= 2) {
-        const float m2 = __shfl_xor(m, o, 64), l2 = __shfl_xor(l, o, 64), e2 = __shfl_xor(e, o, 64);
-        join_stats(m, l, e, m2, l2, e2);
-      }
-    }
-    if (k != 0) continue;
     float own_s = 0.f, own_t = 0.f;
     if (Ks && sl.count) {
       const T* q = Q + b * r.q_user_stride + int64_t(i) * r.d + h * dh;
       const T* o = dO + (b * r.S + i) * r.d + h * dh;
       const int64_t own = ((r.q_user_stride ? b * r.S : 0) + i) * r.d + h * dh;
-      for (int c = 0; c < dh; ++c) {
+      for (int c = k; c < dh; c += LPR) {
         own_s = fmaf(to_f32(q[c]), Ks[own + c], own_s);
         own_t = fmaf(to_f32(o[c]), Vs[own + c], own_t);
       }
-      own_s *= r.scale_log2;
-      join_stats(m, l, e, own_s, 1.f, own_t);
     }
+#pragma unroll
+    for (int o = 1; o < LPR; o *= 2) {
+      const float m2 = __shfl_xor(m, o, 64), l2 = __shfl_xor(l, o, 64), e2 = __shfl_xor(e, o, 64);
+      join_stats(m, l, e, m2, l2, e2);
+      own_s += __shfl_xor(own_s, o, 64);
+      own_t += __shfl_xor(own_t, o, 64);
+    }
+    if (k != 0) continue;
+    own_s *= r.scale_log2;
+    if (Ks && sl.count) join_stats(m, l, e, own_s, 1.f, own_t);
     const float ls = sl.count ? m + __builtin_amdgcn_logf(l) : 0.f, dl = sl.count ? e / l : 0.f;
     lse[at] = ls;
     delta[at] = dl;
@@ -140,7 +141,7 @@ hipError_t join_stats_t(const GradRows& r, const float* stats, int rows, float* 
   if (r.G >= 7 * int64_t(r.B))
     return launch(join_stats_kernel<T, 64>, dim3(blocks_for(total * 64)), dim3(256), 0, s, r, stats, rows, lse, delta,
                   static_cast<const T*>(Q), static_cast<const T*>(dO), Ks, Vs, own_p, own_ds);
-  return launch(join_stats_kernel<T, 1>, dim3(blocks_for(total)), dim3(256), 0, s, r, stats, rows, lse, delta,
+  return launch(join_stats_kernel<T, 8>, dim3(blocks_for(total * 8)), dim3(256), 0, s, r, stats, rows, lse, delta,
                 static_cast<const T*>(Q), static_cast<const T*>(dO), Ks, Vs, own_p, own_ds);
 }
 

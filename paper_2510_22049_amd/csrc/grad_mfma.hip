@@ -588,7 +588,7 @@ int mfma_grad_segment(const vista_summarize_desc& d) {
   const int64_t each = 256 / d.H, k = (d.total_items + each * 32768 - 1) / (each * 32768);
   const int64_t parts = each * (k > 0 ? k : 1);
   const int64_t seg = ((d.total_items + parts - 1) / parts + 31) / 32 * 32;
-  return int(seg < 256 ? 256 : seg);
+  return int(seg < 128 ? 128 : seg);
 }
 
 size_t mfma_summarize_backward_workspace(const vista_summarize_desc& d) { return layout(d).total; }

@@ -219,24 +219,25 @@ __global__ __launch_bounds__(kNormThreads) void norm_backward_kernel(NormParams 
   }
 }
 
-// Columns of the partial rows: 16 columns a workgroup, 16 threads a column, each an ascending run of
-// every sixteenth row, the sixteen added in ascending order.
+// Columns of the partial rows: 16 columns a workgroup, 64 threads a column, each an ascending run of every 64th row, the runs
+// added in ascending order.  (16 threads a column: 7.8 us for 1024 rows of 512 columns, 64: 4.9; latency.)
+constexpr int kRuns = 64;
 template <typename T>
-__global__ __launch_bounds__(256) void norm_columns_kernel(const float* __restrict__ partials, int groups, int d,
-                                                           T* __restrict__ d_weight, T* __restrict__ d_bias) {
-  __shared__ float part[16][17];
+__global__ __launch_bounds__(16 * kRuns) void norm_columns_kernel(const float* __restrict__ partials, int groups, int d,
+                                                                 T* __restrict__ d_weight, T* __restrict__ d_bias) {
+  __shared__ float part[kRuns][17];
   const int c = threadIdx.x & 15, k = threadIdx.x >> 4;
   const int col = blockIdx.x * 16 + c;
   float s = 0.f;
   if (col < 2 * d) {
-#pragma unroll 4
-    for (int g = k; g < groups; g += 16) s += partials[int64_t(g) * 2 * d + col];
+#pragma unroll 8
+    for (int g = k; g < groups; g += kRuns) s += partials[int64_t(g) * 2 * d + col];
   }
   part[k][c] = s;
   __syncthreads();
   if (k == 0 && col < 2 * d) {
-#pragma unroll
-    for (int i = 1; i < 16; ++i) s += part[i][c];
+#pragma unroll 16
+    for (int i = 1; i < kRuns; ++i) s += part[i][c];
     T* out = col < d ? d_weight : d_bias;
     if (out) store_chunk<1>(out + (col < d ? col : col - d), {s});
   }
@@ -320,10 +321,10 @@ vista_status layer_norm_backward(const vista_norm_desc& d, float eps, const void
   if (!sums) return VISTA_OK;
   const dim3 blocks((2 * d.d + 15) / 16);
   if (d.dtype == VISTA_BF16)
-    VISTA_LAUNCH(norm_columns_kernel<bf16_t>, blocks, dim3(256), 0, s, p.partials, int(grid), d.d,
+    VISTA_LAUNCH(norm_columns_kernel<bf16_t>, blocks, dim3(16 * kRuns), 0, s, p.partials, int(grid), d.d,
                  static_cast<bf16_t*>(dw), static_cast<bf16_t*>(db));
   else
-    VISTA_LAUNCH(norm_columns_kernel<float>, blocks, dim3(256), 0, s, p.partials, int(grid), d.d, static_cast<float*>(dw),
+    VISTA_LAUNCH(norm_columns_kernel<float>, blocks, dim3(16 * kRuns), 0, s, p.partials, int(grid), d.d, static_cast<float*>(dw),
                  static_cast<float*>(db));
   return VISTA_OK;
 }
