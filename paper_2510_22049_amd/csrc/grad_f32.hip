@@ -131,14 +131,16 @@ __device__ __forceinline__ void sweep(Others<DT>& o, const TA* a, const TB* b, c
 template <int DT>
 __device__ __forceinline__ f32x4 products(const float* rows, const float4 (&own)[DT]) {
   const int g = (threadIdx.x & 63) >> 4, c = threadIdx.x & 15;
-  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  f32x4 s = {0.f, 0.f, 0.f, 0.f}, t = s;       // two chains: half the latency
 #pragma unroll
   for (int n = 0; n < DT; ++n) {
     const float4 x = *reinterpret_cast<const float4*>(rows + c * Others<DT>::kRow + 16 * n + 4 * g);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) s = mfma4(at(x, i), at(own[n], i), s);
+    s = mfma4(x.x, own[n].x, s);
+    t = mfma4(x.y, own[n].y, t);
+    s = mfma4(x.z, own[n].z, s);
+    t = mfma4(x.w, own[n].w, t);
   }
-  return s;
+  return s + t;
 }
 // acc^T[channel][own] += sum over the 16 rows of row[channel] w[row][own]
 template <int DT>
@@ -268,11 +270,10 @@ struct HistoryGrad {
 
 // Queries' rows over one segment: the statistics of every piece, or (GRAD) its share of dQ.
 template <typename T, int DT, bool GRAD>
-__global__ __launch_bounds__(256) void history_queries_kernel(HistoryGrad p) {
-  __shared__ __align__(16) Others<DT> o;
+__device__ __forceinline__ void history_queries(const HistoryGrad& p, Others<DT>& o, int64_t block, int64_t blocks) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
   const int dh = p.d / p.H;
-  for (int64_t item = blockIdx.x; item < p.G * p.H * p.groups; item += gridDim.x) {
+  for (int64_t item = block; item < p.G * p.H * p.groups; item += blocks) {
     const int64_t segment = item / (p.H * p.groups);
     const int rest = int(item % (p.H * p.groups)), h = rest / p.groups;
     const int i = rest % p.groups * kOwn + 16 * wave + c;
@@ -328,12 +329,11 @@ __global__ __launch_bounds__(256) void history_queries_kernel(HistoryGrad p) {
 // for each of them, with accumulators of its own, so that nothing of one user reaches another's rows.  K and V may be the
 // memory of dK and dV: a wave reads its own rows before it stores them, and nobody else reads them.
 template <typename T, int DT>
-__global__ __launch_bounds__(256) void history_items_kernel(HistoryGrad p) {
-  __shared__ __align__(16) Others<DT> o;
+__device__ __forceinline__ void history_items(const HistoryGrad& p, Others<DT>& o, int64_t block, int64_t blocks) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
   const int dh = p.d / p.H;
-  const int64_t blocks = (p.N + kOwn - 1) / kOwn;
-  for (int64_t item = blockIdx.x; item < blocks * p.H; item += gridDim.x) {
+  const int64_t row_blocks = (p.N + kOwn - 1) / kOwn;
+  for (int64_t item = block; item < row_blocks * p.H; item += blocks) {
     const int64_t begin = item / p.H * kOwn, end = begin + kOwn < p.N ? begin + kOwn : p.N;
     const int h = int(item % p.H);
     const int64_t row = begin + 16 * wave + c;
@@ -371,6 +371,21 @@ __global__ __launch_bounds__(256) void history_items_kernel(HistoryGrad p) {
       }
     }
   }
+}
+
+template <typename T, int DT>
+__global__ __launch_bounds__(256) void history_stats_kernel(HistoryGrad p) {
+  __shared__ __align__(16) Others<DT> o;
+  history_queries<T, DT, false>(p, o, blockIdx.x, gridDim.x);
+}
+// The first `queries` workgroups form dQ, the others dK and dV; with none of one kind it is the other's launch alone.
+template <typename T, int DT>
+__global__ __launch_bounds__(256) void history_grads_kernel(HistoryGrad p, unsigned queries) {
+  __shared__ __align__(16) Others<DT> o;
+  if (blockIdx.x < queries)
+    history_queries<T, DT, true>(p, o, blockIdx.x, queries);
+  else
+    history_items<T, DT>(p, o, blockIdx.x - queries, gridDim.x - queries);
 }
 
 // ------------------------------------------------------------------------------------------------ stage 2
@@ -459,6 +474,105 @@ __global__ __launch_bounds__(256) void candidate_rows_kernel(CandidateGrad p) {
   }
 }
 
+// The same where there are at most 128 summaries: their rows fit LDS together, and a wave keeps scores and dP of its 16 candidates
+// (64 registers) instead of forming them twice.
+constexpr int kShort = 128;
+template <typename T, int DT>
+__global__ __launch_bounds__(256) void candidate_rows_short_kernel(CandidateGrad p) {
+  constexpr int kRow = Others<DT>::kRow, kTiles = kShort / 16;
+  __shared__ __align__(16) float y[kShort * kRow];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
+  const int dh = p.d / p.H;
+  const int64_t groups = (int64_t(p.C) + kOwn - 1) / kOwn, per = p.H * groups;
+  for (int64_t item = blockIdx.x; item < p.B * per; item += gridDim.x) {
+    const int64_t b = item / per;
+    const int h = int(item % per / groups);
+    const int64_t i = item % groups * kOwn + 16 * wave + c;
+    const bool in = i < p.C;
+    const int64_t row = (b * p.C + i) * p.d + h * dh;
+    const T* Y = static_cast<const T*>(p.summ) + b * p.S * p.d + h * dh;
+    float4 q[DT], w[DT];
+    load_own<DT>(q, static_cast<const T*>(p.cand) + row, in, dh, p.wide);
+    load_own<DT>(w, static_cast<const T*>(p.dO) + row, in, dh, p.wide);
+    __syncthreads();                     // the item before has been read
+#pragma unroll 4
+    for (int n = threadIdx.x; n < (p.S + 15) / 16 * 16 * 4 * DT; n += 256) {
+      const int r = n / (4 * DT), ch = n % (4 * DT) * 4;
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (r < p.S) v = load_channels(Y + int64_t(r) * p.d, ch, dh, p.wide);
+      *reinterpret_cast<float4*>(y + r * kRow + ch) = v;
+    }
+    float own_s = 0.f, own_t = 0.f;
+    if (p.self_term) {
+      own_s = own_dot<DT>(q, q) * p.scale_log2;
+      own_t = own_dot<DT>(w, q);
+    }
+    __syncthreads();
+    f32x4 s[kTiles], t[kTiles];
+    float m = kLowest;
+#pragma unroll
+    for (int k = 0; k < kTiles; ++k) {
+      if (16 * k >= p.S) break;
+      s[k] = products<DT>(y + 16 * k * kRow, q) * p.scale_log2;
+      t[k] = products<DT>(y + 16 * k * kRow, w);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[k][r] = 16 * k + 4 * g + r < p.S ? s[k][r] : -__builtin_inff();
+        m = fmaxf(m, s[k][r]);
+      }
+    }
+    m = fmaxf(m, __shfl_xor(m, 16, 64));
+    m = fmaxf(m, __shfl_xor(m, 32, 64));
+    if (p.self_term) m = fmaxf(m, own_s);
+    float l = 0.f, e = 0.f;
+#pragma unroll
+    for (int k = 0; k < kTiles; ++k) {
+      if (16 * k >= p.S) break;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[k][r] = exp2_fast(s[k][r] - m);
+        l += s[k][r];
+        e = fmaf(s[k][r], t[k][r], e);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o < 64; o *= 2) {
+      l += __shfl_xor(l, o, 64);
+      e += __shfl_xor(e, o, 64);
+    }
+    const float own_w = p.self_term ? exp2_fast(own_s - m) : 0.f;
+    l += own_w;
+    e = fmaf(own_w, own_t, e);
+    const float over = 1.f / l, delta = e * over;
+    f32x4 acc[DT];
+    clear(acc);
+#pragma unroll
+    for (int k = 0; k < kTiles; ++k) {
+      if (16 * k >= p.S) break;
+      f32x4 ds;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) ds[r] = 16 * k + 4 * g + r < p.S ? s[k][r] * over * (t[k][r] - delta) : 0.f;
+      add_weighted<DT>(acc, y + 16 * k * kRow, ds);
+    }
+    if (in) {
+      const float pw = own_w * over, ds = 2.f * p.scale * pw * (own_t - delta);
+#pragma unroll
+      for (int n = 0; n < DT; ++n) {
+        f32x4 r = acc[n] * p.scale;
+        if (p.self_term) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) r[k] += fmaf(ds, at(q[n], k), pw * at(w[n], k));
+        }
+        store_channels(static_cast<T*>(p.d_cand) + row, 16 * n + 4 * g, dh, r);
+      }
+      if (g == 0) {
+        p.lse[(b * p.H + h) * p.C + i] = m + __builtin_amdgcn_logf(l);
+        p.delta[(b * p.H + h) * p.C + i] = delta;
+      }
+    }
+  }
+}
+
 // Summaries' rows, 64 a workgroup, over one share of the user's candidates.  Summaries are keys and values: both parts of
 // their gradient go to one accumulator.
 template <typename T, int DT>
@@ -510,15 +624,22 @@ unsigned grid_of(int64_t items) { return unsigned(items < kMostBlocks ? items : 
 
 bool aligned_to(const void* p, size_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
+// The launches of stage 1: statistics, both gradients together (the projections lie apart from the outputs), dQ alone, dK and dV
+// alone.
+enum class Step { kStats, kBoth, kQueries, kItems };
 template <typename T, int DT>
-hipError_t run_history(const HistoryGrad& p, int step, hipStream_t s) {
-  const int64_t queries = p.G * p.H * p.groups, items = (p.N + kOwn - 1) / kOwn * p.H;
-  if (step == 0) return launch(history_queries_kernel<T, DT, false>, dim3(grid_of(queries)), dim3(256), 0, s, p);
-  if (step == 1) return launch(history_queries_kernel<T, DT, true>, dim3(grid_of(queries)), dim3(256), 0, s, p);
-  return launch(history_items_kernel<T, DT>, dim3(grid_of(items)), dim3(256), 0, s, p);
+hipError_t run_history(const HistoryGrad& p, Step step, hipStream_t s) {
+  const unsigned queries = grid_of(p.G * p.H * p.groups), items = grid_of((p.N + kOwn - 1) / kOwn * p.H);
+  const dim3 block(256);
+  switch (step) {
+    case Step::kStats: return launch(history_stats_kernel<T, DT>, dim3(queries), block, 0, s, p);
+    case Step::kBoth: return launch(history_grads_kernel<T, DT>, dim3(queries + items), block, 0, s, p, queries);
+    case Step::kQueries: return launch(history_grads_kernel<T, DT>, dim3(queries), block, 0, s, p, queries);
+    default: return launch(history_grads_kernel<T, DT>, dim3(items), block, 0, s, p, 0u);
+  }
 }
 template <typename T>
-hipError_t history_step(const HistoryGrad& p, int step, hipStream_t s) {
+hipError_t history_step(const HistoryGrad& p, Step step, hipStream_t s) {
   switch ((p.d / p.H + 15) / 16) {
     case 1: return run_history<T, 1>(p, step, s);
     case 2: return run_history<T, 2>(p, step, s);
@@ -530,7 +651,9 @@ hipError_t history_step(const HistoryGrad& p, int step, hipStream_t s) {
 template <typename T, int DT>
 hipError_t run_candidates(const CandidateGrad& p, int step, hipStream_t s) {
   const int64_t rows = p.B * p.H * ((int64_t(p.C) + kOwn - 1) / kOwn), summ = p.B * p.H * p.shares * ((p.S + kOwn - 1) / kOwn);
-  if (step == 0) return launch(candidate_rows_kernel<T, DT>, dim3(grid_of(rows)), dim3(256), 0, s, p);
+  if (step == 0)
+    return p.S <= kShort ? launch(candidate_rows_short_kernel<T, DT>, dim3(grid_of(rows)), dim3(256), 0, s, p)
+                         : launch(candidate_rows_kernel<T, DT>, dim3(grid_of(rows)), dim3(256), 0, s, p);
   return launch(summary_rows_kernel<T, DT>, dim3(grid_of(summ)), dim3(256), 0, s, p);
 }
 template <typename T>
@@ -567,13 +690,18 @@ int f32_grad_segment(const vista_summarize_desc& d) {
 }
 
 namespace {
+// The fp32 projections of the items: in the workspace, so that dQ and dK, dV are one launch (a small call is all latency), or, for
+// fp32 histories of more than 64 MiB of keys, in the memory of the outputs until the items' pass overwrites them.
+bool projections_apart(const vista_summarize_desc& d) {
+  return d.dtype != VISTA_F32 || d.total_items * d.d <= (int64_t(64) << 20) / 4;
+}
 struct HistoryLayout {
   size_t stats, records, rows, self, K, V, Ks, total;   // byte offsets into the workspace
 };
 HistoryLayout history_layout(const vista_summarize_desc& d) {
   const int64_t seg = f32_grad_segment(d), G = (d.total_items + seg - 1) / seg;
   const size_t slots = size_t(G + d.B) * d.H * d.S, rows = size_t(d.B) * d.H * d.S;
-  const size_t kv = d.dtype == VISTA_F32 ? 0 : align256(size_t(d.total_items) * d.d * sizeof(float));
+  const size_t kv = projections_apart(d) ? align256(size_t(d.total_items) * d.d * sizeof(float)) : 0;
   HistoryLayout l;
   l.stats = kHeaderBytes;
   l.records = l.stats + align256(slots * 3 * sizeof(float));
@@ -600,9 +728,9 @@ vista_status f32_summarize_backward(const SummarizeArgs& a, const void* d_out, v
   HistoryGrad p;
   p.Q = a.Q;
   p.dO = d_out;
-  // fp32: the projections wait in the outputs' own memory until the items' pass overwrites them
-  float* K = d.dtype == VISTA_F32 ? static_cast<float*>(d_keys) : floats(l.K);
-  float* V = d.dtype == VISTA_F32 ? static_cast<float*>(d_values) : floats(l.V);
+  const bool apart = projections_apart(d);
+  float* K = apart ? floats(l.K) : static_cast<float*>(d_keys);
+  float* V = apart ? floats(l.V) : static_cast<float*>(d_values);
   p.K = K;
   p.V = V;
   p.offsets = a.offsets;
@@ -628,7 +756,7 @@ vista_status f32_summarize_backward(const SummarizeArgs& a, const void* d_out, v
   p.wide = dh % 4 == 0 && aligned_to(a.Q, 4 * e) && aligned_to(d_out, 4 * e);
   p.wide_kv = dh % 4 == 0 && aligned_to(K, 16) && aligned_to(V, 16);
   const bool bf16 = d.dtype == VISTA_BF16;
-  auto step = [&](int n) { return bf16 ? history_step<bf16_t>(p, n, a.stream) : history_step<float>(p, n, a.stream); };
+  auto step = [&](Step n) { return bf16 ? history_step<bf16_t>(p, n, a.stream) : history_step<float>(p, n, a.stream); };
 
   float *Ks = nullptr, *Vs = nullptr, *own_p = nullptr, *own_ds = nullptr;
   if (d.flags & VISTA_FLAG_SELF_TERM) {
@@ -651,13 +779,15 @@ vista_status f32_summarize_backward(const SummarizeArgs& a, const void* d_out, v
       VISTA_LAUNCH(grad_project_kernel<float>, dim3(grid), dim3(256), 0, a.stream, static_cast<const float*>(a.X),
                    static_cast<const float*>(a.Wk), static_cast<const float*>(a.Wv), K, V, p.N, d.d, row_blocks, col_blocks,
                    wide);
-    if (step(0) != hipSuccess) return VISTA_ERR_HIP;
+    if (step(Step::kStats) != hipSuccess) return VISTA_ERR_HIP;
   }
   const GradRows r = {a.offsets, d.B, d.S, d.d, d.H, a.seg, d.total_items, a.G, a.scale_plain, a.scale_log2, d.q_user_stride,
                       a.offsets_checked ? -1 : d.total_items, reinterpret_cast<int*>(a.workspace)};
   if (grad_join_stats(r, d.dtype, p.stats, d.S, lse, delta, a.Q, d_out, Ks, Vs, own_p, own_ds, a.stream) != hipSuccess)
     return VISTA_ERR_HIP;
-  if (p.N > 0 && (step(1) != hipSuccess || step(2) != hipSuccess)) return VISTA_ERR_HIP;
+  if (p.N > 0 && (apart ? step(Step::kBoth) != hipSuccess
+                        : step(Step::kQueries) != hipSuccess || step(Step::kItems) != hipSuccess))
+    return VISTA_ERR_HIP;
   if (grad_join_queries(r, d.dtype, p.records, d.S, a.scale_plain, a.Q, d_out, Ks, own_p, own_ds, d_queries, d_self_keys, d_self_values,
                         a.stream) != hipSuccess)
     return VISTA_ERR_HIP;
