@@ -157,33 +157,45 @@ def _dev(t: torch.Tensor, name: str) -> int:
     return t.data_ptr()
 
 
-def _shaped(like: torch.Tensor, **tensors) -> None:
-    """Each tensor has the shape it is given with, the type of `like` and its device, which is the current one (the call
-    goes to the current device's stream): a kernel would otherwise read or write past the end of one of them."""
-    if like.is_cuda and like.device.index != torch.cuda.current_device():
+def _shaped(like: torch.Tensor, tensors) -> None:
+    """Each (name, tensor, shape) has that shape, the type of `like` and its device, which is the current one (the call goes to
+    the current device's stream), and is contiguous: a kernel would otherwise read or write past the end of one of them.
+    A tensor that is None is left out."""
+    dtype, index = like.dtype, like.get_device()
+    if index >= 0 and index == _device():
+        for _, t, shape in tensors:              # the usual case: every check at once, half of a small call's host time otherwise
+            if t is not None and (t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous()):
+                break
+        else:
+            return
+    elif index >= 0:
         raise ValueError("the tensors live on another device than the current one")
-    for name, (t, shape) in tensors.items():
+    for name, t, shape in tensors:
         if t is None:
             continue
         if tuple(t.shape) != tuple(shape):
             raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-        if t.dtype != like.dtype:
-            raise TypeError(f"{name} must be {like.dtype}, not {t.dtype}")
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
         if t.device != like.device:
             raise ValueError(f"{name} must live on {like.device}")
+    for name, t, _ in tensors:
+        if t is not None:
+            _dev(t, name)
 
 
 def _workspace(workspace, need, like: torch.Tensor) -> torch.Tensor:
     """The caller's workspace, or one of torch's of need() bytes where there is none."""
     if workspace is None:
         return torch.empty(max(need(), 256), dtype=torch.uint8, device=like.device)
-    if workspace.dtype != torch.uint8 or workspace.device != like.device:
+    if workspace.dtype is not torch.uint8 or workspace.get_device() != like.get_device():
         raise ValueError(f"workspace must be uint8 on {like.device}")
     return workspace
 
 
-def _optional(t, name: str):
-    return None if t is None else _dev(t, name)
+def _at(t):
+    """Address of a tensor that _shaped has checked, or None."""
+    return None if t is None else t.data_ptr()
 
 
 def _stream_getter():
@@ -197,6 +209,7 @@ def _stream_getter():
 
 
 _stream = _stream_getter()
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
 def summarize_desc(B, S, d, H, dtype, total_items, per_user_q=False, scale=0.0, segment_items=0,
@@ -332,10 +345,11 @@ def vista_summarize_backward(history_emb, offsets, virtual_queries, W_k, W_v, d_
     per_user = virtual_queries.dim() == 3
     if (d_self_keys is None) != (d_self_values is None):
         raise ValueError("d_self_keys and d_self_values go together")
-    _shaped(history_emb, history_emb=(history_emb, (N, d)), virtual_queries=(virtual_queries, (B, S, d) if per_user else (S, d)),
-            W_k=(W_k, (d, d)), W_v=(W_v, (d, d)), d_out=(d_out, (B, S, d)), d_queries=(d_queries, (B, S, d)),
-            d_keys=(d_keys, (N, d)), d_values=(d_values, (N, d)), d_self_keys=(d_self_keys, (B, S, d)),
-            d_self_values=(d_self_values, (B, S, d)))
+    items, user, summaries = (N, d), (B, S, d) if per_user else (S, d), (B, S, d)
+    _shaped(history_emb, (("history_emb", history_emb, items), ("virtual_queries", virtual_queries, user), ("W_k", W_k, (d, d)),
+                          ("W_v", W_v, (d, d)), ("d_out", d_out, summaries), ("d_queries", d_queries, summaries),
+                          ("d_keys", d_keys, items), ("d_values", d_values, items), ("d_self_keys", d_self_keys, summaries),
+                          ("d_self_values", d_self_values, summaries)))
     desc = summarize_desc(B, S, d, H, _dtype_code(history_emb), N, per_user, scale, segment_items, VISTA_ATTN_SOFTMAX,
                           d_self_keys is not None)
     host = None
@@ -345,13 +359,11 @@ def vista_summarize_backward(history_emb, offsets, virtual_queries, W_k, W_v, d_
         offsets_host = offsets_host.contiguous()
         host = offsets_host.data_ptr()
     workspace = _workspace(workspace, lambda: lib().vista_summarize_backward_workspace_bytes(C.byref(desc)), history_emb)
-    rows = (lambda t, name: _dev(t, name)) if N else (lambda t, name: None)
-    st = lib().vista_summarize_backward(C.byref(desc), rows(history_emb, "history_emb"), _dev(offsets, "offsets"), host,
-                                        _dev(virtual_queries, "virtual_queries"), _dev(W_k, "W_k"), _dev(W_v, "W_v"),
-                                        _dev(d_out, "d_out"), _dev(d_queries, "d_queries"), rows(d_keys, "d_keys"),
-                                        rows(d_values, "d_values"), _optional(d_self_keys, "d_self_keys"),
-                                        _optional(d_self_values, "d_self_values"), _dev(workspace, "workspace"),
-                                        workspace.numel(), _stream())
+    st = lib().vista_summarize_backward(C.byref(desc), _at(history_emb if N else None), _dev(offsets, "offsets"), host,
+                                        virtual_queries.data_ptr(), W_k.data_ptr(), W_v.data_ptr(), d_out.data_ptr(),
+                                        d_queries.data_ptr(), _at(d_keys if N else None), _at(d_values if N else None),
+                                        _at(d_self_keys), _at(d_self_values), _dev(workspace, "workspace"), workspace.numel(),
+                                        _stream())
     if st != VISTA_OK:
         raise VistaError(st)
     return workspace
@@ -365,14 +377,14 @@ def vista_target_attend_backward(candidates, summaries, d_out, d_candidates, d_s
         raise ValueError("candidates must be [B, C, d] and summaries [B, S, d]")
     B, Cn, d = candidates.shape
     S = summaries.shape[1]
-    _shaped(candidates, candidates=(candidates, (B, Cn, d)), summaries=(summaries, (B, S, d)), d_out=(d_out, (B, Cn, d)),
-            d_candidates=(d_candidates, (B, Cn, d)), d_summaries=(d_summaries, (B, S, d)))
+    cand, summ = (B, Cn, d), (B, S, d)
+    _shaped(candidates, (("candidates", candidates, cand), ("summaries", summaries, summ), ("d_out", d_out, cand),
+                         ("d_candidates", d_candidates, cand), ("d_summaries", d_summaries, summ)))
     desc = AttendDesc(B=B, C=Cn, S=S, d=d, H=H, dtype=_dtype_code(candidates), scale=scale,
                       flags=VISTA_FLAG_SELF_TERM if self_term else 0)
     workspace = _workspace(workspace, lambda: lib().vista_target_attend_backward_workspace_bytes(C.byref(desc)), candidates)
-    st = lib().vista_target_attend_backward(C.byref(desc), _dev(candidates, "candidates"), _dev(summaries, "summaries"),
-                                            _dev(d_out, "d_out"), _dev(d_candidates, "d_candidates"),
-                                            _dev(d_summaries, "d_summaries"), _dev(workspace, "workspace"),
+    st = lib().vista_target_attend_backward(C.byref(desc), candidates.data_ptr(), summaries.data_ptr(), d_out.data_ptr(),
+                                            d_candidates.data_ptr(), d_summaries.data_ptr(), _dev(workspace, "workspace"),
                                             workspace.numel(), _stream())
     if st != VISTA_OK:
         raise VistaError(st)
@@ -450,18 +462,17 @@ def vista_sglu_ffn(y, W_g, W_u, W_o, out, *, eps=0.0):
         raise VistaError(st)
 
 
-def _norm_rows(x: torch.Tensor) -> NormDesc:
+def _norm_desc(x: torch.Tensor, eps: float) -> NormDesc:
     d = x.shape[-1]
-    return NormDesc(rows=x.numel() // d if d else 0, d=d, dtype=_dtype_code(x))
+    return NormDesc(x.numel() // d if d else 0, d, _dtype_code(x), eps)
 
 
 def vista_layer_norm(x, weight, bias, y, *, eps=0.0):
     """Layer norm of the rows of x [..., d] into y (which may be x); weight and bias [d], each may be None."""
-    desc = _norm_rows(x)
-    desc.eps = eps
-    _shaped(x, weight=(weight, (desc.d,)), bias=(bias, (desc.d,)), y=(y, x.shape))
-    st = lib().vista_layer_norm(C.byref(desc), _dev(x, "x"), _optional(weight, "weight"), _optional(bias, "bias"), _dev(y, "y"),
-                                _stream())
+    desc = _norm_desc(x, eps)
+    row = (desc.d,)
+    _shaped(x, (("x", x, x.shape), ("weight", weight, row), ("bias", bias, row), ("y", y, x.shape)))
+    st = lib().vista_layer_norm(C.byref(desc), x.data_ptr(), _at(weight), _at(bias), y.data_ptr(), _stream())
     if st != VISTA_OK:
         raise VistaError(st)
 
@@ -469,16 +480,15 @@ def vista_layer_norm(x, weight, bias, y, *, eps=0.0):
 def vista_layer_norm_backward(x, weight, d_y, d_x, d_weight, d_bias, *, eps=0.0, workspace=None):
     """Gradients of layer norm: d_y [..., d] -> d_x (which may be d_y), d_weight and d_bias [d] (each may be None).  Returns
     the workspace, which may be passed to the next call; None where neither sum is wanted."""
-    desc = _norm_rows(x)
-    desc.eps = eps
-    _shaped(x, weight=(weight, (desc.d,)), d_y=(d_y, x.shape), d_x=(d_x, x.shape), d_weight=(d_weight, (desc.d,)),
-            d_bias=(d_bias, (desc.d,)))
+    desc = _norm_desc(x, eps)
+    row = (desc.d,)
+    _shaped(x, (("x", x, x.shape), ("weight", weight, row), ("d_y", d_y, x.shape), ("d_x", d_x, x.shape),
+                ("d_weight", d_weight, row), ("d_bias", d_bias, row)))
     if d_weight is not None or d_bias is not None:
         workspace = _workspace(workspace, lambda: lib().vista_layer_norm_backward_workspace_bytes(C.byref(desc)), x)
-    st = lib().vista_layer_norm_backward(C.byref(desc), _dev(x, "x"), _optional(weight, "weight"), _dev(d_y, "d_y"),
-                                         _dev(d_x, "d_x"), _optional(d_weight, "d_weight"), _optional(d_bias, "d_bias"),
-                                         _optional(workspace, "workspace"), workspace.numel() if workspace is not None else 0,
-                                         _stream())
+    st = lib().vista_layer_norm_backward(C.byref(desc), x.data_ptr(), _at(weight), d_y.data_ptr(), d_x.data_ptr(), _at(d_weight),
+                                         _at(d_bias), None if workspace is None else _dev(workspace, "workspace"),
+                                         0 if workspace is None else workspace.numel(), _stream())
     if st != VISTA_OK:
         raise VistaError(st)
     return workspace
