@@ -341,9 +341,15 @@ __global__ __launch_bounds__(64 * kStatsWaves, 2) void history_stats_kernel(Hist
 }
 
 // ------------------------------------------------------------------------------------------------ gradients
+// LOW: the keys' low terms are in dQ's product too.  The keys' roundings are independent and average out of the sum over a
+// long history's items, while the gradient's own part grows with it: dQ is off by 2.9e-3 of its norm at 16 items, 2.3e-3 at
+// 4 d, 1.9e-3 at 16 d, of which 1.7e-3 is its rounding to bf16.  With the low terms it is 2.4e-3 at 16 items; they cost
+// 750 us a call instead of 707 (768597 items of 64 users, d = 128, H = 4, S = 256).  So they are there for average histories
+// of less than 4 d items.
 constexpr int kGradWaves = 4;          // one a SIMD: dQ alone is 16 registers for 32 queries
+constexpr int kLongHistory = 4;        // times d
 
-template <int D, int NQB>
+template <int D, int NQB, bool LOW>
 __global__ __launch_bounds__(64 * kGradWaves, 1) void history_grad_kernel(HistoryGradParams p) {
   constexpr int NT = 64 * kGradWaves, KS = D / 16;
   __shared__ __align__(16) char rows[2 * NQB * kBlockBytes];      // Q, dO
@@ -385,7 +391,7 @@ __global__ __launch_bounds__(64 * kGradWaves, 1) void history_grad_kernel(Histor
     for (; t < tiles; t += kGradWaves) {
       const int64_t first = pc.begin + int64_t(t) * 32;
       const int left = pc.end - first < 32 ? int(pc.end - first) : 32;
-      bf16x8 kh[2], kl[2], vh[2], vl[2], kt[2];
+      bf16x8 kh[2], kl[2], vh[2], vl[2], kt[2], kt_low[2];
       {
         f32x16 k, v;
         // the four stores of the last tile's gradients, which followed the request, may still be under way
@@ -394,18 +400,22 @@ __global__ __launch_bounds__(64 * kGradWaves, 1) void history_grad_kernel(Histor
         pack2(k * p.scale_log2, kh, kl);
         // Items past the piece are copies of its last: finite where it is, never stored, and with zeros for keys here they
         // add nothing to dQ.
-        bf16x8 masked[2];
+        auto turn = [&](const bf16x8 (&from)[2], uint32_t offset, bf16x8 (&to)[2]) __attribute__((always_inline)) {
+          bf16x8 masked[2];
 #pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          Pack8 m;
-          m.v = kh[n];
+          for (int n = 0; n < 2; ++n) {
+            Pack8 m;
+            m.v = from[n];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) m.w[i] = l32 < left ? m.w[i] : 0u;
-          masked[n] = m.v;
-        }
-        patch.put(0, masked);
+            for (int i = 0; i < 4; ++i) m.w[i] = l32 < left ? m.w[i] : 0u;
+            masked[n] = m.v;
+          }
+          patch.put(offset, masked);
 #pragma unroll
-        for (int n = 0; n < 2; ++n) kt[n] = patch.get(0, n);
+          for (int n = 0; n < 2; ++n) to[n] = patch.get(offset, n);
+        };
+        turn(kh, 0, kt);
+        if constexpr (LOW) turn(kl, kBlockBytes, kt_low);
         pack2(v, vh, vl);
       }
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the rows have been read
@@ -475,6 +485,7 @@ __global__ __launch_bounds__(64 * kGradWaves, 1) void history_grad_kernel(Histor
           for (int k = 0; k < 2; ++k) {
             dv = mfma(ot[k], w[i][k], qb == 0 && k == 0 ? f32x16{0} : dv);
             dk = mfma(qt[k], dsp[i][k], qb == 0 && k == 0 ? f32x16{0} : dk);
+            if constexpr (LOW) dq[qb] = mfma(kt_low[k], turned[k], dq[qb]);
             dq[qb] = mfma(kt[k], turned[k], dq[qb]);
           }
         }
@@ -489,9 +500,9 @@ __global__ __launch_bounds__(64 * kGradWaves, 1) void history_grad_kernel(Histor
           }
           __builtin_amdgcn_sched_group_barrier(0x100, 12, 0);
 #pragma unroll
-          for (int i = 0; i < 6; ++i) {
+          for (int i = 0; i < (LOW ? 8 : 6); ++i) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, LOW ? 4 : 5, 0);
           }
           __builtin_amdgcn_sched_group_barrier(0x200, 4, 0);
         }
@@ -539,8 +550,9 @@ __global__ __launch_bounds__(64 * kGradWaves, 1) void history_grad_kernel(Histor
 template <int D, int NQB>
 hipError_t run_blocks(const HistoryGradParams& p, bool grad, hipStream_t s) {
   const dim3 grid(segment_blocks(p.G, p.H));
-  return grad ? launch(history_grad_kernel<D, NQB>, grid, dim3(64 * kGradWaves), 0, s, p)
-              : launch(history_stats_kernel<D, NQB>, grid, dim3(64 * kStatsWaves), 0, s, p);
+  if (!grad) return launch(history_stats_kernel<D, NQB>, grid, dim3(64 * kStatsWaves), 0, s, p);
+  return p.N < int64_t(kLongHistory) * D * p.B ? launch(history_grad_kernel<D, NQB, true>, grid, dim3(64 * kGradWaves), 0, s, p)
+                                               : launch(history_grad_kernel<D, NQB, false>, grid, dim3(64 * kGradWaves), 0, s, p);
 }
 // The kernels know how many blocks of 32 queries there are; a call takes the next larger count that is built.
 template <int D>
