@@ -85,9 +85,9 @@ __global__ __launch_bounds__(64, 1) void attend_grad_kernel(AttendGradParams p) 
   __shared__ __align__(16) char patches[2 * kBlockBytes];       // dS and P of a block: reads of one precede writes of the next
   const int lane = threadIdx.x, l32 = lane & 31, hf = lane >> 5;
   // the heads and shares of a user, which read the same lines, run on one XCD one after another
-  const int64_t r = blockIdx.x >> 3;
-  const int per = p.H * p.shares, h = int(r % per) % p.H, share = int(r % per) / p.H;
-  const int64_t b = r / per * 8 + (blockIdx.x & 7);
+  const int64_t unit = int64_t(blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+  const int per = p.H * p.shares, h = int(unit % per) % p.H, share = int(unit % per) / p.H;
+  const int64_t b = unit / per;
   if (b >= p.B) return;
   const int64_t begin = int64_t(share) * p.rows_each, end = begin + p.rows_each < p.C ? begin + p.rows_each : p.C;
   const uint16_t* Y = p.summ + b * p.S * p.d + 32 * h;
@@ -389,7 +389,7 @@ int shares_of(const vista_attend_desc& d) {
 
 template <int NKB, int FULL>
 hipError_t run(const AttendGradParams& p, hipStream_t s) {
-  const dim3 grid(unsigned((p.B + 7) / 8 * 8 * p.H * p.shares));
+  const dim3 grid(unsigned((p.B * p.H * p.shares + 7) / 8 * 8));
   return p.S == 32 * NKB ? launch(attend_grad_kernel<NKB, NKB>, grid, dim3(64), 0, s, p)
                          : launch(attend_grad_kernel<NKB, FULL>, grid, dim3(64), 0, s, p);
 }

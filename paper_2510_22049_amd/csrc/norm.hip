@@ -20,27 +20,28 @@ constexpr int kNormThreads = 256;
 constexpr int kNormWaves = kNormThreads / 64;
 constexpr int kNormGroups = 1024;      // most partial rows of the gradients: four workgroups a compute unit
 
-// A chunk as one load or store: VEC * sizeof(T) is 2, 4 or 16 bytes and the address a multiple of that.
-template <typename T, int VEC>
+// A chunk as one load or store of 16 bytes (of one element where VEC is 1).  ALIGN is what the address is a multiple of:
+// global memory takes any multiple of the element.
+template <typename T, int VEC, int ALIGN>
 __device__ __forceinline__ void load_chunk(const T* p, float (&out)[VEC]) {
-  struct alignas(sizeof(T) * VEC) Raw { T v[VEC]; };
+  struct __attribute__((packed, aligned(ALIGN))) Raw { T v[VEC]; };
   const Raw r = *reinterpret_cast<const Raw*>(p);
 #pragma unroll
   for (int e = 0; e < VEC; ++e) out[e] = to_f32(r.v[e]);
 }
-template <int VEC>
+template <int VEC, int ALIGN>
 __device__ __forceinline__ void store_chunk(float* p, const float (&v)[VEC]) {
-  struct alignas(4 * VEC) Raw { float v[VEC]; } r;
+  struct __attribute__((packed, aligned(ALIGN))) Raw { float v[VEC]; } r;
 #pragma unroll
   for (int e = 0; e < VEC; ++e) r.v[e] = v[e];
   *reinterpret_cast<Raw*>(p) = r;
 }
-template <int VEC>
+template <int VEC, int ALIGN>
 __device__ __forceinline__ void store_chunk(bf16_t* p, const float (&v)[VEC]) {
   if constexpr (VEC == 1) {
     p->bits = uint16_t(pair_to_bf16(v[0], 0.f));
   } else {
-    struct alignas(2 * VEC) Raw { uint32_t v[VEC / 2]; } r;
+    struct __attribute__((packed, aligned(ALIGN))) Raw { uint32_t v[VEC / 2]; } r;
 #pragma unroll
     for (int e = 0; e < VEC / 2; ++e) r.v[e] = pair_to_bf16(v[2 * e], v[2 * e + 1]);
     *reinterpret_cast<Raw*>(p) = r;
@@ -64,16 +65,27 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 
-// LPR lanes a row, CPL chunks of VEC elements a lane: chunk lane + LPR j of the row, j < CPL.
-template <typename T, int VEC, int LPR, int CPL>
+// LPR lanes a row, CPL chunks of VEC elements a lane: chunk lane + LPR j of the row, j < CPL.  WHOLE: rows are whole chunks at
+// aligned addresses.  Otherwise the row's last chunk is its last VEC elements; those that the chunk before holds as well count
+// once in sums and are stored twice, alike.
+template <typename T, int VEC, int LPR, int CPL, bool WHOLE>
 struct Row {
+  static constexpr int kAlign = WHOLE ? VEC * sizeof(T) : sizeof(T);
   float v[CPL][VEC];
+  static __device__ __forceinline__ bool in(int at, int j, int d) { return (at + LPR * j) * VEC < d; }
+  static __device__ __forceinline__ int first(int at, int j, int d) {
+    const int c = (at + LPR * j) * VEC;
+    return WHOLE || c + VEC <= d ? c : d - VEC;
+  }
+  // whether element e of a chunk that is in the row is its own
+  static __device__ __forceinline__ bool own(int at, int j, int e, int d) {
+    return WHOLE || first(at, j, d) + e >= (at + LPR * j) * VEC;
+  }
   __device__ __forceinline__ void load(const T* row, int at, int d) {
 #pragma unroll
     for (int j = 0; j < CPL; ++j) {
-      const int c = (at + LPR * j) * VEC;
-      if (c < d) {
-        load_chunk<T, VEC>(row + c, v[j]);
+      if (in(at, j, d)) {
+        load_chunk<T, VEC, kAlign>(row + first(at, j, d), v[j]);
       } else {
 #pragma unroll
         for (int e = 0; e < VEC; ++e) v[j][e] = 0.f;
@@ -82,10 +94,8 @@ struct Row {
   }
   __device__ __forceinline__ void store(T* row, int at, int d) const {
 #pragma unroll
-    for (int j = 0; j < CPL; ++j) {
-      const int c = (at + LPR * j) * VEC;
-      if (c < d) store_chunk<VEC>(row + c, v[j]);
-    }
+    for (int j = 0; j < CPL; ++j)
+      if (in(at, j, d)) store_chunk<VEC, kAlign>(row + first(at, j, d), v[j]);
   }
   // v -> z; returns r.  Lanes beyond the row's end hold zeros before and after.
   __device__ __forceinline__ float normalise(int at, int d, float inv_d, float eps) {
@@ -93,16 +103,17 @@ struct Row {
 #pragma unroll
     for (int j = 0; j < CPL; ++j)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) s += v[j][e];
+      for (int e = 0; e < VEC; ++e) s += own(at, j, e, d) ? v[j][e] : 0.f;
     const float mean = group_sum<LPR>(s) * inv_d;
     float q = 0.f;
 #pragma unroll
     for (int j = 0; j < CPL; ++j) {
-      const bool in = (at + LPR * j) * VEC < d;
+      const bool inside = in(at, j, d);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
-        v[j][e] = in ? v[j][e] - mean : 0.f;
-        q = fmaf(v[j][e], v[j][e], q);
+        v[j][e] = inside ? v[j][e] - mean : 0.f;
+        const float x = own(at, j, e, d) ? v[j][e] : 0.f;
+        q = fmaf(x, x, q);
       }
     }
     // v_rsq_f32 is within one unit of the last place
@@ -127,19 +138,20 @@ struct NormParams {
   float eps;
 };
 
-template <typename T, int VEC, int LPR, int CPL>
+template <typename T, int VEC, int LPR, int CPL, bool WHOLE>
 __global__ __launch_bounds__(kNormThreads) void norm_kernel(NormParams p) {
   constexpr int kRows = 64 / LPR;        // rows a wave holds
   const int lane = threadIdx.x & 63, at = lane % LPR, sub = lane / LPR;
   const T* X = static_cast<const T*>(p.x);
   T* Y = static_cast<T*>(p.out);
   const float inv_d = 1.f / float(p.d);
-  Row<T, VEC, LPR, CPL> w, b;
+  using R = Row<T, VEC, LPR, CPL, WHOLE>;
+  R w, b;
   if (p.w) w.load(static_cast<const T*>(p.w), at, p.d);
   if (p.b) b.load(static_cast<const T*>(p.b), at, p.d);
   const int64_t stride = int64_t(gridDim.x) * kNormWaves * kRows;
   for (int64_t r = (int64_t(blockIdx.x) * kNormWaves + (threadIdx.x >> 6)) * kRows + sub; r < p.rows; r += stride) {
-    Row<T, VEC, LPR, CPL> x;
+    R x;
     x.load(X + r * p.d, at, p.d);
     x.normalise(at, p.d, inv_d, p.eps);
 #pragma unroll
@@ -155,7 +167,7 @@ __global__ __launch_bounds__(kNormThreads) void norm_kernel(NormParams p) {
   }
 }
 
-template <typename T, int VEC, int LPR, int CPL>
+template <typename T, int VEC, int LPR, int CPL, bool WHOLE>
 __global__ __launch_bounds__(kNormThreads) void norm_backward_kernel(NormParams p) {
   constexpr int kRows = 64 / LPR;
   const int lane = threadIdx.x & 63, at = lane % LPR, sub = lane / LPR;
@@ -164,12 +176,13 @@ __global__ __launch_bounds__(kNormThreads) void norm_backward_kernel(NormParams 
   const T* DY = static_cast<const T*>(p.dy);
   T* DX = static_cast<T*>(p.out);
   const float inv_d = 1.f / float(p.d);
-  Row<T, VEC, LPR, CPL> w;
+  using R = Row<T, VEC, LPR, CPL, WHOLE>;
+  R w;
   if (p.w) w.load(static_cast<const T*>(p.w), at, p.d);
   float dw[CPL][VEC] = {}, db[CPL][VEC] = {};
   const int64_t stride = int64_t(gridDim.x) * kNormWaves * kRows;
   for (int64_t r = (int64_t(blockIdx.x) * kNormWaves + wave) * kRows + sub; r < p.rows; r += stride) {
-    Row<T, VEC, LPR, CPL> x, g;
+    R x, g;
     x.load(X + r * p.d, at, p.d);
     g.load(DY + r * p.d, at, p.d);
     const float rs = x.normalise(at, p.d, inv_d, p.eps);
@@ -181,8 +194,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_backward_kernel(NormParams 
         dw[j][e] = fmaf(g.v[j][e], x.v[j][e], dw[j][e]);
         db[j][e] += g.v[j][e];
         if (p.w) g.v[j][e] *= w.v[j][e];
-        s += g.v[j][e];
-        t = fmaf(g.v[j][e], x.v[j][e], t);
+        const float u = R::own(at, j, e, p.d) ? g.v[j][e] : 0.f;
+        s += u;
+        t = fmaf(u, x.v[j][e], t);
       }
     s = group_sum<LPR>(s) * inv_d;
     t = group_sum<LPR>(t) * inv_d;
@@ -204,9 +218,9 @@ __global__ __launch_bounds__(kNormThreads) void norm_backward_kernel(NormParams 
         dw[j][e] += __shfl_xor(dw[j][e], o, 64);
         db[j][e] += __shfl_xor(db[j][e], o, 64);
       }
-      if (sub == 0) {
-        sums[wave][0][(at + LPR * j) * VEC + e] = dw[j][e];
-        sums[wave][1][(at + LPR * j) * VEC + e] = db[j][e];
+      if (sub == 0 && R::in(at, j, p.d) && R::own(at, j, e, p.d)) {
+        sums[wave][0][R::first(at, j, p.d) + e] = dw[j][e];
+        sums[wave][1][R::first(at, j, p.d) + e] = db[j][e];
       }
     }
   __syncthreads();
@@ -239,17 +253,20 @@ __global__ __launch_bounds__(16 * kRuns) void norm_columns_kernel(const float* _
 #pragma unroll 16
     for (int i = 1; i < kRuns; ++i) s += part[i][c];
     T* out = col < d ? d_weight : d_bias;
-    if (out) store_chunk<1>(out + (col < d ? col : col - d), {s});
+    if (out) store_chunk<1, sizeof(T)>(out + (col < d ? col : col - d), {s});
   }
 }
 
-// Elements a lane moves at a time: as many as divide the width and suit every pointer's alignment.
-int norm_vector(int dtype, int d, const void* const (&ptrs)[6]) {
+// Whether a row is whole chunks of 16 bytes at addresses that are multiples of 16.
+bool norm_whole(int dtype, int d, const void* const (&ptrs)[4]) {
   uintptr_t low = 0;
   for (const void* q : ptrs) low |= reinterpret_cast<uintptr_t>(q);
-  const int size = dtype == VISTA_BF16 ? 2 : 4;
-  if (d * size % 16 == 0 && (low & 15) == 0) return 16 / size;
-  return size == 2 && d % 2 == 0 && (low & 3) == 0 ? 2 : 1;
+  return d * (dtype == VISTA_BF16 ? 2 : 4) % 16 == 0 && (low & 15) == 0;
+}
+// Elements of a chunk: 16 bytes, unless the row has fewer.
+int norm_vector(int dtype, int d) {
+  const int vec = dtype == VISTA_BF16 ? 8 : 4;
+  return d < vec ? 1 : vec;
 }
 
 int norm_lanes(int d, int vec) {
@@ -263,37 +280,33 @@ unsigned norm_grid(int64_t rows, int lanes, int most) {
   return unsigned(need < most ? need : most);
 }
 
-template <typename T, int VEC, int LPR, int CPL>
+template <typename T, int VEC, int LPR, int CPL, bool WHOLE>
 hipError_t run_norm(const NormParams& p, bool backward, unsigned grid, hipStream_t s) {
-  return backward ? launch(norm_backward_kernel<T, VEC, LPR, CPL>, dim3(grid), dim3(kNormThreads), 0, s, p)
-                  : launch(norm_kernel<T, VEC, LPR, CPL>, dim3(grid), dim3(kNormThreads), 0, s, p);
+  return backward ? launch(norm_backward_kernel<T, VEC, LPR, CPL, WHOLE>, dim3(grid), dim3(kNormThreads), 0, s, p)
+                  : launch(norm_kernel<T, VEC, LPR, CPL, WHOLE>, dim3(grid), dim3(kNormThreads), 0, s, p);
 }
 
-// CPL for widths up to kNormMaxWidth = 1024, by the chunk's size
-template <typename T, int VEC>
+// CPL for widths up to kNormMaxWidth = 1024: 128 chunks of bf16, 256 of fp32
+template <typename T, int VEC, bool WHOLE>
 hipError_t pick_norm(const NormParams& p, bool backward, unsigned grid, int lanes, hipStream_t s) {
   const int chunks = (p.d + VEC - 1) / VEC;
-  if (lanes == 8) return run_norm<T, VEC, 8, 1>(p, backward, grid, s);
-  if (lanes == 16) return run_norm<T, VEC, 16, 1>(p, backward, grid, s);
-  if (lanes == 32) return run_norm<T, VEC, 32, 1>(p, backward, grid, s);
-  if (chunks <= 64) return run_norm<T, VEC, 64, 1>(p, backward, grid, s);
-  if (chunks <= 128) return run_norm<T, VEC, 64, 2>(p, backward, grid, s);
-  if constexpr (VEC <= 4) {
-    if (chunks <= 256) return run_norm<T, VEC, 64, 4>(p, backward, grid, s);
+  if (lanes == 8) return run_norm<T, VEC, 8, 1, WHOLE>(p, backward, grid, s);
+  if (lanes == 16) return run_norm<T, VEC, 16, 1, WHOLE>(p, backward, grid, s);
+  if (lanes == 32) return run_norm<T, VEC, 32, 1, WHOLE>(p, backward, grid, s);
+  if (chunks <= 64) return run_norm<T, VEC, 64, 1, WHOLE>(p, backward, grid, s);
+  if (chunks <= 128) return run_norm<T, VEC, 64, 2, WHOLE>(p, backward, grid, s);
+  if constexpr (VEC == 4) {
+    if (chunks <= 256) return run_norm<T, VEC, 64, 4, WHOLE>(p, backward, grid, s);
   }
-  if constexpr (VEC <= 2) {
-    if (chunks <= 512) return run_norm<T, VEC, 64, 8>(p, backward, grid, s);
-  }
-  if constexpr (VEC == 1) return run_norm<T, VEC, 64, 16>(p, backward, grid, s);
   return hipErrorInvalidValue;
 }
 
-hipError_t dispatch_norm(const NormParams& p, int dtype, int vec, bool backward, unsigned grid, int lanes, hipStream_t s) {
-  if (dtype == VISTA_BF16)
-    return vec == 8   ? pick_norm<bf16_t, 8>(p, backward, grid, lanes, s)
-           : vec == 2 ? pick_norm<bf16_t, 2>(p, backward, grid, lanes, s)
-                      : pick_norm<bf16_t, 1>(p, backward, grid, lanes, s);
-  return vec == 4 ? pick_norm<float, 4>(p, backward, grid, lanes, s) : pick_norm<float, 1>(p, backward, grid, lanes, s);
+template <typename T>
+hipError_t dispatch_norm(const NormParams& p, int vec, bool whole, bool backward, unsigned grid, int lanes, hipStream_t s) {
+  constexpr int kVec = 16 / sizeof(T);
+  return vec == 1 ? run_norm<T, 1, 8, 1, true>(p, backward, grid, s)
+         : whole  ? pick_norm<T, kVec, true>(p, backward, grid, lanes, s)
+                  : pick_norm<T, kVec, false>(p, backward, grid, lanes, s);
 }
 
 }  // namespace
@@ -301,10 +314,13 @@ hipError_t dispatch_norm(const NormParams& p, int dtype, int vec, bool backward,
 vista_status layer_norm(const vista_norm_desc& d, float eps, const void* x, const void* w, const void* b, void* y,
                         hipStream_t s) {
   if (d.rows == 0) return VISTA_OK;
-  const int vec = norm_vector(d.dtype, d.d, {x, w, b, y, nullptr, nullptr}), lanes = norm_lanes(d.d, vec);
+  const int vec = norm_vector(d.dtype, d.d), lanes = norm_lanes(d.d, vec);
+  const bool whole = norm_whole(d.dtype, d.d, {x, w, b, y});
   const NormParams p = {x, w, b, nullptr, y, nullptr, d.rows, d.d, eps};
-  return dispatch_norm(p, d.dtype, vec, false, norm_grid(d.rows, lanes, 8 * 256), lanes, s) == hipSuccess ? VISTA_OK
-                                                                                                         : VISTA_ERR_HIP;
+  const unsigned grid = norm_grid(d.rows, lanes, 8 * 256);
+  const hipError_t e = d.dtype == VISTA_BF16 ? dispatch_norm<bf16_t>(p, vec, whole, false, grid, lanes, s)
+                                             : dispatch_norm<float>(p, vec, whole, false, grid, lanes, s);
+  return e == hipSuccess ? VISTA_OK : VISTA_ERR_HIP;
 }
 
 size_t layer_norm_backward_workspace(const vista_norm_desc& d) {
@@ -313,11 +329,16 @@ size_t layer_norm_backward_workspace(const vista_norm_desc& d) {
 
 vista_status layer_norm_backward(const vista_norm_desc& d, float eps, const void* x, const void* w, const void* dy,
                                  void* dx, void* dw, void* db, void* workspace, hipStream_t s) {
-  const int vec = norm_vector(d.dtype, d.d, {x, w, dy, dx, nullptr, nullptr}), lanes = norm_lanes(d.d, vec);
+  const int vec = norm_vector(d.dtype, d.d), lanes = norm_lanes(d.d, vec);
+  const bool whole = norm_whole(d.dtype, d.d, {x, w, dy, dx});
   const bool sums = dw || db;
   const NormParams p = {x, w, nullptr, dy, dx, sums ? static_cast<float*>(workspace) : nullptr, d.rows, d.d, eps};
   const unsigned grid = norm_grid(d.rows, lanes, kNormGroups);
-  if (grid && dispatch_norm(p, d.dtype, vec, true, grid, lanes, s) != hipSuccess) return VISTA_ERR_HIP;
+  if (grid) {
+    const hipError_t e = d.dtype == VISTA_BF16 ? dispatch_norm<bf16_t>(p, vec, whole, true, grid, lanes, s)
+                                               : dispatch_norm<float>(p, vec, whole, true, grid, lanes, s);
+    if (e != hipSuccess) return VISTA_ERR_HIP;
+  }
   if (!sums) return VISTA_OK;
   const dim3 blocks((2 * d.d + 15) / 16);
   if (d.dtype == VISTA_BF16)
