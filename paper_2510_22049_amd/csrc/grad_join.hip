@@ -69,27 +69,50 @@ __global__ __launch_bounds__(256) void join_stats_kernel(GradRows r, const float
   }
 }
 
-// RUNS threads a column (1 or 8), each an interleaved ascending run, added in ascending order.
-template <typename T, int RUNS>
+template <typename T, int V>
+__device__ __forceinline__ void store_grads(T* p, const float (&v)[V]) {
+  if constexpr (V == 1) {
+    store_grad(p, v[0]);
+  } else if constexpr (sizeof(T) == 2) {
+    struct __attribute__((packed, aligned(2))) Raw { uint32_t v[V / 2]; } r;
+#pragma unroll
+    for (int e = 0; e < V / 2; ++e) r.v[e] = pair_to_bf16(v[2 * e], v[2 * e + 1]);
+    *reinterpret_cast<Raw*>(p) = r;
+  } else {
+    struct __attribute__((packed, aligned(4))) Raw { float v[V]; } r;
+#pragma unroll
+    for (int e = 0; e < V; ++e) r.v[e] = v[e];
+    *reinterpret_cast<Raw*>(p) = r;
+  }
+}
+
+// V columns a thread (4 where they divide the head's width: a quarter of the index arithmetic, which is most of this kernel; 18 us
+// with single columns for 64 users of 256 x 128).  RUNS threads for the same columns (1 or 8), each an interleaved ascending
+// run, added in ascending order.
+template <typename T, int RUNS, int V>
 __global__ __launch_bounds__(256) void join_queries_kernel(GradRows r, const float* __restrict__ records, int rows, float factor,
                                                            const T* Q, const T* dO, const float* Ks, const float* own_p,
                                                            const float* own_ds, T* d_queries, T* d_self_keys, T* d_self_values) {
   constexpr int kCols = 256 / RUNS;
-  __shared__ float part[RUNS][kCols];
-  const int64_t total = int64_t(r.B) * r.S * r.d;
+  struct alignas(4 * V) Chunk { float v[V]; };
+  __shared__ Chunk part[RUNS][kCols];
+  const int64_t total = int64_t(r.B) * r.S * r.d / V;
   const int c = threadIdx.x % kCols, k = threadIdx.x / kCols, dh = r.d / r.H;
   for (int64_t base = int64_t(blockIdx.x) * kCols; base < total; base += int64_t(gridDim.x) * kCols) {
-    const int64_t at = base + c;
-    const bool in = at < total;
-    const int64_t row = in ? at / r.d : 0, b = row / r.S;
-    const int i = int(row % r.S), col = in ? int(at % r.d) : 0, h = col / dh;
+    const bool in = base + c < total;
+    const int64_t at = (base + c) * V, row = in ? at / r.d : 0, b = row / r.S;
+    const int i = int(row - b * r.S), col = in ? int(at - row * r.d) : 0, h = col / dh;
     const Slots sl = slots_of(r, b);
-    float sum = 0.f;
+    Chunk sum = {};
     if (in) {
-      const float* rec = records + ((sl.first * r.H + h) * rows + i) * dh + col % dh;
+      const float* rec = records + ((sl.first * r.H + h) * rows + i) * dh + (col - h * dh);
       const int64_t step = int64_t(r.H) * rows * dh;
 #pragma unroll 4
-      for (int64_t n = k; n < sl.count; n += RUNS) sum += rec[n * step];
+      for (int64_t n = k; n < sl.count; n += RUNS) {
+        const Chunk one = *reinterpret_cast<const Chunk*>(rec + n * step);
+#pragma unroll
+        for (int e = 0; e < V; ++e) sum.v[e] += one.v[e];
+      }
     }
     if (RUNS > 1) {
       __syncthreads();
@@ -97,19 +120,28 @@ __global__ __launch_bounds__(256) void join_queries_kernel(GradRows r, const flo
       __syncthreads();
       if (k == 0)
 #pragma unroll
-        for (int n = 1; n < RUNS; ++n) sum += part[n][c];
+        for (int n = 1; n < RUNS; ++n)
+#pragma unroll
+          for (int e = 0; e < V; ++e) sum.v[e] += part[n][c].v[e];
     }
     if (!in || k != 0) continue;
-    sum *= factor;
+#pragma unroll
+    for (int e = 0; e < V; ++e) sum.v[e] *= factor;
     if (Ks) {
       const int64_t stat = (b * r.H + h) * r.S + i, own = ((r.q_user_stride ? b * r.S : 0) + i) * r.d + col;
       const bool any = sl.count != 0;
-      const float ds = any ? own_ds[stat] * r.scale : 0.f;
-      if (any) sum = fmaf(ds, Ks[own], sum);
-      store_grad(d_self_keys + at, any ? ds * to_f32(Q[b * r.q_user_stride + int64_t(i) * r.d + col]) : 0.f);
-      store_grad(d_self_values + at, any ? own_p[stat] * to_f32(dO[at]) : 0.f);
+      const float ds = any ? own_ds[stat] * r.scale : 0.f, p = any ? own_p[stat] : 0.f;
+      float dk[V], dv[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        if (any) sum.v[e] = fmaf(ds, Ks[own + e], sum.v[e]);
+        dk[e] = any ? ds * to_f32(Q[b * r.q_user_stride + int64_t(i) * r.d + col + e]) : 0.f;
+        dv[e] = any ? p * to_f32(dO[at + e]) : 0.f;
+      }
+      store_grads<T, V>(d_self_keys + at, dk);
+      store_grads<T, V>(d_self_values + at, dv);
     }
-    store_grad(d_queries + at, sum);
+    store_grads<T, V>(d_queries + at, sum.v);
   }
 }
 
@@ -149,14 +181,14 @@ template <typename T>
 hipError_t join_queries_t(const GradRows& r, const float* records, int rows, float factor, const void* Q, const void* dO,
                           const float* Ks, const float* own_p, const float* own_ds, void* dq, void* dks, void* dvs,
                           hipStream_t s) {
-  const int64_t total = int64_t(r.B) * r.S * r.d;
-  if (r.G >= 7 * int64_t(r.B))
-    return launch(join_queries_kernel<T, 8>, dim3(blocks_for(total * 8)), dim3(256), 0, s, r, records, rows, factor,
-                  static_cast<const T*>(Q), static_cast<const T*>(dO), Ks, own_p, own_ds, static_cast<T*>(dq),
-                  static_cast<T*>(dks), static_cast<T*>(dvs));
-  return launch(join_queries_kernel<T, 1>, dim3(blocks_for(total)), dim3(256), 0, s, r, records, rows, factor,
-                static_cast<const T*>(Q), static_cast<const T*>(dO), Ks, own_p, own_ds, static_cast<T*>(dq),
-                static_cast<T*>(dks), static_cast<T*>(dvs));
+  auto run = [&](auto* kernel, int runs, int columns) {
+    const int64_t threads = int64_t(r.B) * r.S * r.d / columns * runs;
+    return launch(kernel, dim3(blocks_for(threads)), dim3(256), 0, s, r, records, rows, factor, static_cast<const T*>(Q),
+                  static_cast<const T*>(dO), Ks, own_p, own_ds, static_cast<T*>(dq), static_cast<T*>(dks), static_cast<T*>(dvs));
+  };
+  const bool many = r.G >= 7 * int64_t(r.B);
+  if (r.d / r.H % 4 == 0) return many ? run(join_queries_kernel<T, 8, 4>, 8, 4) : run(join_queries_kernel<T, 1, 4>, 1, 4);
+  return many ? run(join_queries_kernel<T, 8, 1>, 8, 1) : run(join_queries_kernel<T, 1, 1>, 1, 1);
 }
 
 }  // namespace
