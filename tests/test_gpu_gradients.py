@@ -189,6 +189,13 @@ def test_history_gradients_of_long_histories():
     assert all(torch.equal(a[k], b[k]) for k in a)
 
 
+@pytest.mark.parametrize("d,H,S", [(64, 2, 100), (64, 2, 384), (128, 4, 256), (128, 4, 20), (256, 8, 70), (256, 8, 512)])
+@pytest.mark.parametrize("less", [0, 1])
+def test_history_gradients_on_either_side_of_an_average_of_4_d_items(d, H, S, less):
+    p = History(9, [7 * d - less, d], d, H, S, "bf16", per_user=True)
+    p.check(p.run())
+
+
 # ------------------------------------------------------------------------------------------------ stage 2
 class Candidates:
     def __init__(self, seed, B, C, d, H, S, dtype, self_term=False, scale=0.0, std=1.0):
@@ -278,6 +285,26 @@ def test_random_gradients(seed):
     p.check(p.run(int(g.choice([0, 0, 64, 96])), host=bool(g.random() < 0.5)))
     c = Candidates(seed, int(g.integers(1, 6)), int(g.integers(1, 400)), H * dh, H, S, dtype, self_term)
     c.check(c.run())
+
+
+def test_calls_on_two_streams_with_a_workspace_each():
+    jobs = [History(31, [900, 40, 0, 2000], 128, 4, 96, "bf16", True, True), History(32, [500, 700], 64, 1, 30, "f32")]
+    once = [j.run() for j in jobs]
+    spaces = [j.ws for j in jobs]
+    streams = [torch.cuda.Stream() for _ in jobs]
+    args = []
+    for j, first in zip(jobs, once):
+        out = {k: torch.full_like(t, float("nan")) for k, t in first.items()}
+        args.append(([dev(j.X, j.dtype), torch.from_numpy(j.off).cuda(), *(dev(a, j.dtype) for a in (j.Q, j.Wk, j.Wv, j.dO))], out))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for j, s, ws, (given, out) in zip(jobs, streams, spaces, args):
+            with torch.cuda.stream(s):
+                V.vista_summarize_backward(*given, out["dQ"], out["dK"], out["dV"], H=j.H, workspace=ws,
+                                           d_self_keys=out.get("dKs"), d_self_values=out.get("dVs"))
+    torch.cuda.synchronize()
+    for first, (_, out) in zip(once, args):
+        assert all(torch.equal(first[k], out[k]) for k in first)
 
 
 # ------------------------------------------------------------------------------------------------ differences of the forward calls

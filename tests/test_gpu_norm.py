@@ -91,6 +91,22 @@ def test_many_rows_sum_in_place_and_repeatable():
         assert np.linalg.norm(host64(got) - want) <= 2.4e-3 * np.linalg.norm(want)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 211), ("bf16", 999), ("f32", 67), ("bf16", 9)])
+def test_rows_that_are_no_whole_chunks_in_place(dtype, d):
+    """A row's last chunk overlaps the one before: in place it has been read before either is stored."""
+    g = np.random.default_rng(d)
+    rows = 5003
+    x, w, b, dy = (rnd(g, s, dtype) for s in ((rows, d), (d,), (d,), (rows, d)))
+    X, W, Bt, DY = (dev(a, dtype) for a in (x, w, b, dy))
+    y, dx = torch.empty_like(X), torch.empty_like(X)
+    sums = [torch.empty_like(W) for _ in range(4)]
+    V.vista_layer_norm(X, W, Bt, y)
+    V.vista_layer_norm_backward(X, W, DY, dx, *sums[:2])
+    V.vista_layer_norm_backward(X, W, DY, DY, *sums[2:])
+    V.vista_layer_norm(X, W, Bt, X)
+    assert torch.equal(X, y) and torch.equal(DY, dx) and torch.equal(sums[0], sums[2]) and torch.equal(sums[1], sums[3])
+
+
 def test_rows_of_one_value_and_rows_that_are_not_finite():
     x = torch.randn(6, 128, device="cuda")
     clean = torch.empty_like(x)
