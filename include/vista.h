@@ -341,7 +341,9 @@ vista_status vista_qla_backward(const vista_summarize_desc* desc,
  *   workspace       >= vista_summarize_backward_workspace_bytes(desc), 256-byte aligned; status word as in vista_summarize.
  *                   It holds nothing between calls; calls that may overlap in time need one each.
  * No output overlaps an input or another output.  Equal calls give equal bits.
- * Supported: every shape and dtype vista_summarize takes; tensors aligned to their elements.
+ * Supported: every shape and dtype vista_summarize takes; tensors aligned to their elements.  bf16 with heads of width 32 in a
+ * model of width 64, 128 or 256 takes the bf16 matrix cores where history_emb, virtual_queries, d_out, d_keys and d_values are
+ * aligned to 16 bytes; everything else the fp32 ones.
  */
 size_t vista_summarize_backward_workspace_bytes(const vista_summarize_desc* desc);
 vista_status vista_summarize_backward(const vista_summarize_desc* desc,
@@ -370,7 +372,8 @@ vista_status vista_summarize_backward(const vista_summarize_desc* desc,
  *   d_out, d_candidates  device [B, C, d] dtype     d_summaries  device [B, S, d] dtype
  *   workspace            >= vista_target_attend_backward_workspace_bytes(desc), 256-byte aligned; nothing is kept in it
  * No output overlaps an input or another output.  Equal calls give equal bits.
- * Supported: every shape and dtype vista_target_attend takes; tensors aligned to their elements.
+ * Supported: every shape and dtype vista_target_attend takes; tensors aligned to their elements.  bf16 with heads of width 32 takes
+ * the bf16 matrix cores where all five tensors are aligned to 16 bytes; everything else the fp32 ones.
  */
 size_t vista_target_attend_backward_workspace_bytes(const vista_attend_desc* desc);
 vista_status vista_target_attend_backward(const vista_attend_desc* desc,

@@ -17,7 +17,14 @@
 // vector work of block n - 1 and gradients of block n - 2 share a step.
 //
 // Roundings.  scale log2(e) Q is taken as two bf16 terms (one would move a score s by 2^-9 s); P and dS are rounded to
-// bf16 once each, their errors independent; everything else is exact or fp32.
+// bf16 once each, their errors independent; everything else is exact or fp32.  Against fp64, 2-norm: 2.3e-3 to 2.4e-3, of which
+// 1.7e-3 is the output's rounding.
+//
+// Measured, 1024 users x 512 candidates, d = 128, H = 4, S = 256: 400 us a call in a stream, 206 GFLOP of the definition, at 2.05 GHz;
+// 18 products of 32x32x16 a unit of 32 candidates x 32 summaries, 12 of them the definition's, are 144 us of the matrix pipe, and
+// 32 exponentials and some 90 plain vector instructions a lane and unit nearly as much of the vector unit; the rest is what a wave
+// alone on its SIMD waits for: a tile's start and its statistics between the walks.  With a mask on every block instead of the last
+// few: 459.  Two users x 100 candidates: 15.5 us, one tile a wave, of which most is code that is walked once.
 #include "grad_mfma.hpp"
 
 namespace vista {

@@ -14,6 +14,10 @@
 // That is seven products of the history's gradient where five and the two of the statistics would do, and no
 // exchange between waves: on these instructions (157 TFLOP/s) the products are what a call waits for.
 // Head widths that are no multiple of 16 are padded with zeros on their way into LDS and registers.
+//
+// Measured: one user of 1024 items, d = 64, one head, 16 queries, fp32: 32 us, five launches of 4 to 11 us, all latency.  75 users x 333
+// candidates, d = 64, one head, 100 summaries, with the self term: 61 us: 26 for candidates' rows, 34 for summaries' rows, of which 13
+// are their products, the rest loads that two steps of 32 candidates cannot hide; 5 for the join.
 #include "common.hpp"
 #include "grad.hpp"
 
