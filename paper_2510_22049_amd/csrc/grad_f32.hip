@@ -16,8 +16,8 @@
 // Head widths that are no multiple of 16 are padded with zeros on their way into LDS and registers.
 //
 // Measured: one user of 1024 items, d = 64, one head, 16 queries, fp32: 32 us, five launches of 4 to 11 us, all latency.  75 users x 333
-// candidates, d = 64, one head, 100 summaries, with the self term: 61 us: 26 for candidates' rows, 34 for summaries' rows, of which 13
-// are their products, the rest loads that two steps of 32 candidates cannot hide; 5 for the join.
+// candidates, d = 64, one head, 100 summaries, with the self term: 41 us, 5 of them the join; 61 with a pass for the
+// candidates' rows and one for the summaries' rows, each forming scores and dP (as beyond 128 summaries).
 #include "common.hpp"
 #include "grad.hpp"
 
@@ -478,102 +478,160 @@ __global__ __launch_bounds__(256) void candidate_rows_kernel(CandidateGrad p) {
   }
 }
 
-// The same where there are at most 128 summaries: their rows fit LDS together, and a wave keeps scores and dP of its 16 candidates
-// (64 registers) instead of forming them twice.
+// Both gradients where there are at most 128 summaries: their rows fit LDS together, and a wave keeps scores and dP of its 16
+// candidates (64 registers), so that each product is formed once.  A workgroup takes a share of one user's head, 64 candidates at a
+// time; dY of 64 candidates is formed from dS, then P, of all four waves, which take the summaries' rows dY (accumulators for the
+// whole share) lies in turn by 16.  The weights pass through LDS where the summaries' rows were.
 constexpr int kShort = 128;
 template <typename T, int DT>
-__global__ __launch_bounds__(256) void candidate_rows_short_kernel(CandidateGrad p) {
-  constexpr int kRow = Others<DT>::kRow, kTiles = kShort / 16;
-  __shared__ __align__(16) float y[kShort * kRow];
+__global__ __launch_bounds__(256, 2) void candidates_short_kernel(CandidateGrad p) {
+  constexpr int kRow = Others<DT>::kRow, kTiles = kShort / 16, kWeights = kOwn + 4;
+  __shared__ __align__(16) float y[kShort * kWeights];            // summaries' rows, then weights [summary][candidate]
+  __shared__ __align__(16) float rows[2][kOwn * kRow];            // candidates, d_out
+  static_assert(kRow <= kWeights, "summaries' rows fit the weights' place");
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
-  const int dh = p.d / p.H;
-  const int64_t groups = (int64_t(p.C) + kOwn - 1) / kOwn, per = p.H * groups;
+  const int dh = p.d / p.H, tiles = (p.S + 15) / 16;
+  const int64_t per = int64_t(p.H) * p.shares;
   for (int64_t item = blockIdx.x; item < p.B * per; item += gridDim.x) {
     const int64_t b = item / per;
-    const int h = int(item % per / groups);
-    const int64_t i = item % groups * kOwn + 16 * wave + c;
-    const bool in = i < p.C;
-    const int64_t row = (b * p.C + i) * p.d + h * dh;
+    const int share = int(item % per) / p.H, h = int(item % per) % p.H;
+    const int64_t begin = int64_t(share) * p.rows_each, end = begin + p.rows_each < p.C ? begin + p.rows_each : p.C;
     const T* Y = static_cast<const T*>(p.summ) + b * p.S * p.d + h * dh;
-    float4 q[DT], w[DT];
-    load_own<DT>(q, static_cast<const T*>(p.cand) + row, in, dh, p.wide);
-    load_own<DT>(w, static_cast<const T*>(p.dO) + row, in, dh, p.wide);
-    __syncthreads();                     // the item before has been read
+    f32x4 dy[2][DT];
+    clear(dy[0]);
+    clear(dy[1]);
+    for (int64_t first = begin; first < end; first += kOwn) {
+      const int64_t i = first + 16 * wave + c;
+      const bool in = i < end;
+      const int64_t row = (b * p.C + i) * p.d + h * dh;
+      float4 q[DT], w[DT];
+      load_own<DT>(q, static_cast<const T*>(p.cand) + row, in, dh, p.wide);      // zeros beyond the share: nothing for dY
+      load_own<DT>(w, static_cast<const T*>(p.dO) + row, in, dh, p.wide);
+      __syncthreads();                   // the candidates before have been read
 #pragma unroll 4
-    for (int n = threadIdx.x; n < (p.S + 15) / 16 * 16 * 4 * DT; n += 256) {
-      const int r = n / (4 * DT), ch = n % (4 * DT) * 4;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (r < p.S) v = load_channels(Y + int64_t(r) * p.d, ch, dh, p.wide);
-      *reinterpret_cast<float4*>(y + r * kRow + ch) = v;
-    }
-    float own_s = 0.f, own_t = 0.f;
-    if (p.self_term) {
-      own_s = own_dot<DT>(q, q) * p.scale_log2;
-      own_t = own_dot<DT>(w, q);
-    }
-    __syncthreads();
-    f32x4 s[kTiles], t[kTiles];
-    float m = kLowest;
-#pragma unroll
-    for (int k = 0; k < kTiles; ++k) {
-      if (16 * k >= p.S) break;
-      s[k] = products<DT>(y + 16 * k * kRow, q) * p.scale_log2;
-      t[k] = products<DT>(y + 16 * k * kRow, w);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        s[k][r] = 16 * k + 4 * g + r < p.S ? s[k][r] : -__builtin_inff();
-        m = fmaxf(m, s[k][r]);
+      for (int n = threadIdx.x; n < tiles * 16 * 4 * DT; n += 256) {
+        const int r = n / (4 * DT), ch = n % (4 * DT) * 4;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < p.S) v = load_channels(Y + int64_t(r) * p.d, ch, dh, p.wide);
+        *reinterpret_cast<float4*>(y + r * kRow + ch) = v;
       }
-    }
-    m = fmaxf(m, __shfl_xor(m, 16, 64));
-    m = fmaxf(m, __shfl_xor(m, 32, 64));
-    if (p.self_term) m = fmaxf(m, own_s);
-    float l = 0.f, e = 0.f;
-#pragma unroll
-    for (int k = 0; k < kTiles; ++k) {
-      if (16 * k >= p.S) break;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        s[k][r] = exp2_fast(s[k][r] - m);
-        l += s[k][r];
-        e = fmaf(s[k][r], t[k][r], e);
-      }
-    }
-#pragma unroll
-    for (int o = 16; o < 64; o *= 2) {
-      l += __shfl_xor(l, o, 64);
-      e += __shfl_xor(e, o, 64);
-    }
-    const float own_w = p.self_term ? exp2_fast(own_s - m) : 0.f;
-    l += own_w;
-    e = fmaf(own_w, own_t, e);
-    const float over = 1.f / l, delta = e * over;
-    f32x4 acc[DT];
-    clear(acc);
-#pragma unroll
-    for (int k = 0; k < kTiles; ++k) {
-      if (16 * k >= p.S) break;
-      f32x4 ds;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) ds[r] = 16 * k + 4 * g + r < p.S ? s[k][r] * over * (t[k][r] - delta) : 0.f;
-      add_weighted<DT>(acc, y + 16 * k * kRow, ds);
-    }
-    if (in) {
-      const float pw = own_w * over, ds = 2.f * p.scale * pw * (own_t - delta);
 #pragma unroll
       for (int n = 0; n < DT; ++n) {
-        f32x4 r = acc[n] * p.scale;
-        if (p.self_term) {
+        *reinterpret_cast<float4*>(rows[0] + (16 * wave + c) * kRow + 16 * n + 4 * g) = q[n];
+        *reinterpret_cast<float4*>(rows[1] + (16 * wave + c) * kRow + 16 * n + 4 * g) = w[n];
+      }
+      float own_s = 0.f, own_t = 0.f;
+      if (p.self_term) {
+        own_s = own_dot<DT>(q, q) * p.scale_log2;
+        own_t = own_dot<DT>(w, q);
+      }
+      __syncthreads();
+      f32x4 s[kTiles], t[kTiles];
+      float m = kLowest;
+      int left = p.S - 4 * g;
+      asm volatile("" : "+v"(left));     // compared here, not once before the loop: 32 masks do not fit the scalar registers
 #pragma unroll
-          for (int k = 0; k < 4; ++k) r[k] += fmaf(ds, at(q[n], k), pw * at(w[n], k));
+      for (int k = 0; k < kTiles; ++k) {
+        if (k >= tiles) break;
+        s[k] = products<DT>(y + 16 * k * kRow, q) * p.scale_log2;
+        t[k] = products<DT>(y + 16 * k * kRow, w);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[k][r] = 16 * k + r < left ? s[k][r] : -__builtin_inff();
+          m = fmaxf(m, s[k][r]);
         }
-        store_channels(static_cast<T*>(p.d_cand) + row, 16 * n + 4 * g, dh, r);
       }
-      if (g == 0) {
-        p.lse[(b * p.H + h) * p.C + i] = m + __builtin_amdgcn_logf(l);
-        p.delta[(b * p.H + h) * p.C + i] = delta;
+      m = fmaxf(m, __shfl_xor(m, 16, 64));
+      m = fmaxf(m, __shfl_xor(m, 32, 64));
+      if (p.self_term) m = fmaxf(m, own_s);
+      float l = 0.f, e = 0.f;
+#pragma unroll
+      for (int k = 0; k < kTiles; ++k) {
+        if (k >= tiles) break;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[k][r] = exp2_fast(s[k][r] - m);
+          l += s[k][r];
+          e = fmaf(s[k][r], t[k][r], e);
+        }
       }
+#pragma unroll
+      for (int o = 16; o < 64; o *= 2) {
+        l += __shfl_xor(l, o, 64);
+        e += __shfl_xor(e, o, 64);
+      }
+      const float own_w = p.self_term ? exp2_fast(own_s - m) : 0.f;
+      l += own_w;
+      e = fmaf(own_w, own_t, e);
+      const float over = 1.f / l, delta = e * over;
+      f32x4 acc[DT];
+      clear(acc);
+#pragma unroll
+      for (int k = 0; k < kTiles; ++k) {
+        if (k >= tiles) break;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          s[k][r] *= over;                // 0 beyond S, and dP there is 0 as well
+          t[k][r] = s[k][r] * (t[k][r] - delta) * p.scale;
+        }
+        add_weighted<DT>(acc, y + 16 * k * kRow, t[k]);
+      }
+      if (in) {
+        const float pw = own_w * over, ds = 2.f * p.scale * pw * (own_t - delta);
+#pragma unroll
+        for (int n = 0; n < DT; ++n) {
+          f32x4 r = acc[n];
+          if (p.self_term) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) r[k] += fmaf(ds, at(q[n], k), pw * at(w[n], k));
+          }
+          store_channels(static_cast<T*>(p.d_cand) + row, 16 * n + 4 * g, dh, r);
+        }
+      }
+      // dY[summary][channel] += weights[summary][candidate] rows[candidate][channel]
+      auto add = [&](const f32x4 (&v)[kTiles], const float* of) __attribute__((always_inline)) {
+        __syncthreads();                 // what lies there has been read
+#pragma unroll
+        for (int k = 0; k < kTiles; ++k) {
+          if (k >= tiles) break;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) y[(16 * k + 4 * g + r) * kWeights + 16 * wave + c] = v[k][r];
+        }
+        __syncthreads();
+        if (wave >= tiles) return;
+        const bool both = wave + 4 < tiles;
+        const float* mine = y + (16 * wave + c) * kWeights + 4 * g;
+#pragma unroll
+        for (int j = 0; j < kOwn / 16; ++j) {
+          const float4 a = *reinterpret_cast<const float4*>(mine + 16 * j);
+          float4 a2 = a;
+          if (both) a2 = *reinterpret_cast<const float4*>(mine + 64 * kWeights + 16 * j);
+#pragma unroll
+          for (int n = 0; n < DT; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const float x = of[(16 * j + 4 * g + r) * kRow + 16 * n + c];
+              dy[0][n] = mfma4(at(a, r), x, dy[0][n]);
+              if (both) dy[1][n] = mfma4(at(a2, r), x, dy[1][n]);
+            }
+        }
+      };
+      add(t, rows[0]);
+      add(s, rows[1]);
     }
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int n = 0; n < DT; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int i = 16 * (wave + 4 * k) + 4 * g + r, ch = 16 * n + c;
+          if (i >= p.S || ch >= dh) continue;
+          if (p.shares == 1)
+            store_grad(static_cast<T*>(p.d_summ) + (b * p.S + i) * p.d + h * dh + ch, dy[k][n][r]);
+          else
+            p.records[(((int64_t(share) * p.B + b) * p.H + h) * p.S + i) * dh + ch] = dy[k][n][r];
+        }
   }
 }
 
@@ -655,9 +713,9 @@ hipError_t history_step(const HistoryGrad& p, Step step, hipStream_t s) {
 template <typename T, int DT>
 hipError_t run_candidates(const CandidateGrad& p, int step, hipStream_t s) {
   const int64_t rows = p.B * p.H * ((int64_t(p.C) + kOwn - 1) / kOwn), summ = p.B * p.H * p.shares * ((p.S + kOwn - 1) / kOwn);
-  if (step == 0)
-    return p.S <= kShort ? launch(candidate_rows_short_kernel<T, DT>, dim3(grid_of(rows)), dim3(256), 0, s, p)
-                         : launch(candidate_rows_kernel<T, DT>, dim3(grid_of(rows)), dim3(256), 0, s, p);
+  if (p.S <= kShort)
+    return step == 0 ? launch(candidates_short_kernel<T, DT>, dim3(grid_of(p.B * p.H * p.shares)), dim3(256), 0, s, p) : hipSuccess;
+  if (step == 0) return launch(candidate_rows_kernel<T, DT>, dim3(grid_of(rows)), dim3(256), 0, s, p);
   return launch(summary_rows_kernel<T, DT>, dim3(grid_of(summ)), dim3(256), 0, s, p);
 }
 template <typename T>
@@ -672,11 +730,12 @@ hipError_t candidates_step(const CandidateGrad& p, int step, hipStream_t s) {
 
 size_t align256(size_t v) { return (v + 255) & ~size_t(255); }
 
-// Shares of a user's candidates in the summaries' pass: so many that some 1024 workgroups have work, 64 candidates or
-// more each.
+// Shares of a user's candidates in the summaries' pass: so many that some 1024 workgroups have work, or the 512 that run at a time
+// where one pass does everything, 64 candidates or more each.
 int candidate_shares(const vista_attend_desc& d) {
-  const int64_t base = int64_t(d.B) * d.H * ((d.S + kOwn - 1) / kOwn), most = (int64_t(d.C) + 63) / 64;
-  const int64_t want = (1024 + base - 1) / base;
+  const bool one = d.S <= kShort;
+  const int64_t base = int64_t(d.B) * d.H * (one ? 1 : (d.S + kOwn - 1) / kOwn), most = (int64_t(d.C) + kOwn - 1) / kOwn;
+  const int64_t want = ((one ? 512 : 1024) + base - 1) / base;
   return int(want < most ? want : most);
 }
 
@@ -801,14 +860,14 @@ vista_status f32_summarize_backward(const SummarizeArgs& a, const void* d_out, v
 // ------------------------------------------------------------------------------------------------ stage 2, host side
 
 size_t f32_attend_backward_workspace(const vista_attend_desc& d) {
-  const size_t rows = size_t(d.B) * d.H * d.C, shares = candidate_shares(d);
+  const size_t shares = candidate_shares(d), rows = d.S <= kShort ? 1 : size_t(d.B) * d.H * d.C;
   return 2 * align256(rows * sizeof(float)) + (shares > 1 ? align256(shares * d.B * d.S * d.d * sizeof(float)) : 0);
 }
 
 vista_status f32_attend_backward(const vista_attend_desc& d, float scale, const void* cand, const void* summ, const void* d_out,
                                  void* d_cand, void* d_summ, void* workspace, hipStream_t s) {
-  const size_t e = d.dtype == VISTA_F32 ? 4 : 2, rows = size_t(d.B) * d.H * d.C;
-  const int dh = d.d / d.H;
+  const size_t e = d.dtype == VISTA_F32 ? 4 : 2, rows = d.S <= kShort ? 1 : size_t(d.B) * d.H * d.C;
+  const int dh = d.d / d.H, unit = d.S <= kShort ? kOwn : kOthers;
   CandidateGrad p;
   p.cand = cand;
   p.summ = summ;
@@ -824,7 +883,7 @@ vista_status f32_attend_backward(const vista_attend_desc& d, float scale, const 
   p.d = d.d;
   p.H = d.H;
   p.shares = candidate_shares(d);
-  p.rows_each = int(((int64_t(d.C) + p.shares - 1) / p.shares + kOthers - 1) / kOthers * kOthers);
+  p.rows_each = int(((int64_t(d.C) + p.shares - 1) / p.shares + unit - 1) / unit * unit);
   p.shares = int((int64_t(d.C) + p.rows_each - 1) / p.rows_each);
   p.scale = scale;
   p.scale_log2 = scale * kLog2e;

@@ -236,6 +236,18 @@ def test_candidate_gradients(dtype, B, C, d, H, S, self_term):
     p.check(p.run())
 
 
+@pytest.mark.parametrize("B,C,d,H,S", [
+    (3, 63, 64, 1, 1), (2, 65, 48, 1, 16), (1, 700, 64, 2, 63), (600, 70, 32, 2, 112), (5, 128, 33, 1, 127), (300, 200, 64, 1, 128),
+    (2, 129, 64, 4, 129), (1, 1, 7, 7, 65)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_candidate_gradients_around_128_summaries(dtype, B, C, d, H, S):
+    p = Candidates(16, B, C, d, H, S, dtype, self_term=B % 2 == 1)
+    a = p.run()
+    p.check(a, users=sorted({0, B // 2, B - 1}))
+    b = p.run(ws=p.ws.fill_(255))
+    assert all(torch.equal(a[k], b[k]) for k in a)
+
+
 @pytest.mark.parametrize("self_term", [False, True])
 @pytest.mark.parametrize("B,C,d,H,S", [
     (1, 1, 32, 1, 1), (2, 100, 128, 4, 256), (3, 31, 64, 2, 100), (2, 64, 128, 4, 64), (1, 5000, 128, 4, 256),
