@@ -19,8 +19,9 @@ __device__ __forceinline__ Slots slots_of(const GradRows& r, int64_t b) {
   return {g0 + b, g1 - g0 + 1};
 }
 
-// LPR lanes a row (8 or 64): lane k joins every LPR-th record from its k-th on, and takes every LPR-th channel of the own key's
-// products.  (One thread a row: 20 us instead of 5 where 9600 rows have a key of their own.)
+// LPR lanes a row (1, 8 or 64): lane k joins every LPR-th record from its k-th on, and takes every LPR-th channel of the own key's
+// products.  (One thread a row: 20 us instead of 5 where 9600 rows have a key of
+// their own; eight: 50 instead of 9 for a million rows of one record each and none.)
 template <typename T, int LPR>
 __global__ __launch_bounds__(256) void join_stats_kernel(GradRows r, const float* __restrict__ stats, int rows,
                                                          float* __restrict__ lse, float* __restrict__ delta, const T* Q,
@@ -169,7 +170,10 @@ template <typename T>
 hipError_t join_stats_t(const GradRows& r, const float* stats, int rows, float* lse, float* delta, const void* Q, const void* dO,
                         const float* Ks, const float* Vs, float* own_p, float* own_ds, hipStream_t s) {
   const int64_t total = int64_t(r.B) * r.H * r.S;
-  // a wave a row once users hold eight records or more
+  // a lane a row where users hold less than two records and have no key of their own, a wave once they hold eight or more
+  if (r.G < r.B && !Ks)
+    return launch(join_stats_kernel<T, 1>, dim3(blocks_for(total)), dim3(256), 0, s, r, stats, rows, lse, delta,
+                  static_cast<const T*>(Q), static_cast<const T*>(dO), Ks, Vs, own_p, own_ds);
   if (r.G >= 7 * int64_t(r.B))
     return launch(join_stats_kernel<T, 64>, dim3(blocks_for(total * 64)), dim3(256), 0, s, r, stats, rows, lse, delta,
                   static_cast<const T*>(Q), static_cast<const T*>(dO), Ks, Vs, own_p, own_ds);

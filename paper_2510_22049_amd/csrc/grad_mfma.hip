@@ -317,27 +317,37 @@ __global__ __launch_bounds__(64 * kStatsWaves, 2) void history_stats_kernel(Hist
       });
       fresh = false;
     }
-    // the two halves of a query, then the waves in ascending order, through the memory of the rows' operands
+    // the two halves of a query, then the waves that had a tile in ascending order, eight blocks at a time through the memory of the
+    // items' rows
+    constexpr int kAtOnce = NQB < 8 ? NQB : 8;
+    static_assert(kAtOnce * 32 * 3 * sizeof(float) <= Items<D>::kBytes, "a wave's statistics fit its rows' place");
     const int64_t slot = (segment + pc.user) * p.H + h;
-    auto joined = [&](int w, int k) { return reinterpret_cast<float*>(xs[w]) + 32 * k; };
-    each<NQB>([&](auto block) __attribute__((always_inline)) {
-      constexpr int qb = decltype(block)::value;
-      if (wave >= tiles) m[qb] = kLowest;            // a wave without a tile has no reference
-      const float m2 = __shfl_xor(m[qb], 32, 64), l2 = __shfl_xor(l[qb], 32, 64), e2 = __shfl_xor(e[qb], 32, 64);
-      join_stats(m[qb], l[qb], e[qb], m2, l2, e2);
+    const int active = tiles < kStatsWaves ? tiles : kStatsWaves;
+    auto joined = [&](int w, int i) { return reinterpret_cast<float*>(xs[w]) + 3 * i; };
+    each<(NQB + kAtOnce - 1) / kAtOnce>([&](auto part) __attribute__((always_inline)) {
+      constexpr int from = decltype(part)::value * kAtOnce, count = NQB - from < kAtOnce ? NQB - from : kAtOnce;
+      if (from > 0) __syncthreads();
+      if (wave < active)
+        each<count>([&](auto block) __attribute__((always_inline)) {
+          constexpr int n = decltype(block)::value, qb = from + n;
+          const float m2 = __shfl_xor(m[qb], 32, 64), l2 = __shfl_xor(l[qb], 32, 64), e2 = __shfl_xor(e[qb], 32, 64);
+          join_stats(m[qb], l[qb], e[qb], m2, l2, e2);
+          if (hf == 0) {
+            float* at = joined(wave, 32 * n + l32);
+            at[0] = m[qb];
+            at[1] = l[qb];
+            at[2] = e[qb];
+          }
+        });
       __syncthreads();
-      if (hf == 0) {
-        joined(wave, 0)[l32] = m[qb];
-        joined(wave, 1)[l32] = l[qb];
-        joined(wave, 2)[l32] = e[qb];
-      }
-      __syncthreads();
-      const int i = 32 * qb + int(threadIdx.x);
-      if (threadIdx.x < 32 && i < p.S) {
-        float jm = joined(0, 0)[l32], jl = joined(0, 1)[l32], je = joined(0, 2)[l32];
-#pragma unroll
-        for (int w = 1; w < kStatsWaves; ++w) join_stats(jm, jl, je, joined(w, 0)[l32], joined(w, 1)[l32], joined(w, 2)[l32]);
-        float* out = p.stats + (slot * p.S + i) * 3;
+      for (int n = threadIdx.x; n < 32 * count && 32 * from + n < p.S; n += NT) {
+        const float* first = joined(0, n);
+        float jm = first[0], jl = first[1], je = first[2];
+        for (int w = 1; w < active; ++w) {
+          const float* at = joined(w, n);
+          join_stats(jm, jl, je, at[0], at[1], at[2]);
+        }
+        float* out = p.stats + (slot * p.S + 32 * from + n) * 3;
         out[0] = jm;
         out[1] = jl;
         out[2] = je;
@@ -525,24 +535,39 @@ __global__ __launch_bounds__(64 * kGradWaves, 1) void history_grad_kernel(Histor
         }
       }
     }
-    // dQ of the piece: 32 queries at a time every wave lays its sums down, [query][channel] in fp32, and a part of each wave's
-    // threads adds them up in ascending order
+    // dQ of the piece: 32 queries at a time every wave that had a tile lays its sums down, [query][channel] in fp32, and a part of
+    // each wave's threads adds them up in ascending order
+    const int active = tiles < kGradWaves ? tiles : kGradWaves;
+    // One wave's sums need no adding up: straight to memory (not beside 16 blocks, whose registers are spilled for it: 804 us instead
+    // of 745 for 200003 items, d = 256, S = 512).  1024 users of 50 items each, S = 256, d = 128: 235 -> 213 us of this kernel.
     float* rec = p.records + ((segment + pc.user) * p.H + h) * int64_t(p.rows) * 32;
+    if (NQB < 16 && active == 1) {
+      if (wave == 0)
+        each<NQB>([&](auto block) __attribute__((always_inline)) {
+          constexpr int qb = decltype(block)::value;
+          if (32 * qb < p.rows)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+              *reinterpret_cast<float4*>(rec + (32 * qb + l32) * 32 + 8 * g + 4 * hf) =
+                  make_float4(dq[qb][4 * g], dq[qb][4 * g + 1], dq[qb][4 * g + 2], dq[qb][4 * g + 3]);
+        });
+      continue;
+    }
     each<NQB>([&](auto block) __attribute__((always_inline)) {
       constexpr int qb = decltype(block)::value;
       __syncthreads();
+      if (wave < active)
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int c = 2 * g + hf;        // 16-byte chunk of the query's row: channels 8 g + 4 hf on
-        *reinterpret_cast<float4*>(patches[wave] + l32 * 128 + ((c ^ (l32 & 7)) << 4)) =
-            make_float4(dq[qb][4 * g], dq[qb][4 * g + 1], dq[qb][4 * g + 2], dq[qb][4 * g + 3]);
-      }
+        for (int g = 0; g < 4; ++g) {
+          const int c = 2 * g + hf;      // 16-byte chunk of the query's row: channels 8 g + 4 hf on
+          *reinterpret_cast<float4*>(patches[wave] + l32 * 128 + ((c ^ (l32 & 7)) << 4)) =
+              make_float4(dq[qb][4 * g], dq[qb][4 * g + 1], dq[qb][4 * g + 2], dq[qb][4 * g + 3]);
+        }
       __syncthreads();
       for (int i = threadIdx.x; i < 256 && 32 * qb < p.rows; i += NT) {
         const int row = i / 8, c = i % 8;
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int w = 0; w < kGradWaves; ++w) {
+        for (int w = 0; w < active; ++w) {
           const float4 v = *reinterpret_cast<const float4*>(patches[w] + row * 128 + ((c ^ (row & 7)) << 4));
           sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
         }
@@ -600,13 +625,15 @@ bool mfma_summarize_backward_supported(const vista_summarize_desc& d) {
 }
 
 // A workgroup is one (segment, head); one fits a compute unit.  Segments that make one round of 256 workgroups, at most 32768 items
-// and at least 256 (a tile for every wave).
+// and at least 128, a tile for every wave, or, where users have fewer items than that and a segment's pieces cost more than its
+// tiles, 32.  (98 users of 539 items together, S = 512, d = 256: 400 us instead of 1400.)
 int mfma_grad_segment(const vista_summarize_desc& d) {
   if (d.segment_items > 0) return d.segment_items;
   const int64_t each = 256 / d.H, k = (d.total_items + each * 32768 - 1) / (each * 32768);
   const int64_t parts = each * (k > 0 ? k : 1);
   const int64_t seg = ((d.total_items + parts - 1) / parts + 31) / 32 * 32;
-  return int(seg < 128 ? 128 : seg);
+  const int64_t least = d.total_items < 128 * int64_t(d.B) ? 32 : 128;
+  return int(seg < least ? least : seg);
 }
 
 size_t mfma_summarize_backward_workspace(const vista_summarize_desc& d) { return layout(d).total; }

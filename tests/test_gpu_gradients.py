@@ -180,6 +180,16 @@ def test_offsets_that_are_wrong_are_reported(dtype, d, H, S):
     assert int(p.ws[:4].view(torch.int32).item()) == V.VISTA_ERR_OFFSETS
 
 
+@pytest.mark.parametrize("d,H,S,self_term", [(64, 2, 40, False), (128, 4, 256, False), (128, 4, 100, True), (256, 8, 512, False), (48, 3, 20, False)])
+def test_history_gradients_of_many_short_histories(d, H, S, self_term):
+    g = np.random.default_rng(40)
+    p = History(10, [int(x) for x in g.integers(0, 66, size=60)] + [200], d, H, S, "bf16", self_term=self_term)
+    a = p.run()
+    p.check(a)
+    b = p.run(ws=p.ws.fill_(255))
+    assert all(torch.equal(a[k], b[k]) for k in a)
+
+
 def test_history_gradients_of_long_histories():
     """More segments than the device has places for, one user over many of them: split, joined, repeatable."""
     p = History(8, [50_000, 3, 9000], 128, 4, 64, "bf16")
