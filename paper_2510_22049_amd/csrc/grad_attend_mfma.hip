@@ -20,11 +20,11 @@
 // bf16 once each, their errors independent; everything else is exact or fp32.  Against fp64, 2-norm: 2.3e-3 to 2.4e-3, of which
 // 1.7e-3 is the output's rounding.
 //
-// Measured, 1024 users x 512 candidates, d = 128, H = 4, S = 256: 400 us a call in a stream, 206 GFLOP of the definition, at 2.05 GHz;
+// Measured, 1024 users x 512 candidates, d = 128, H = 4, S = 256: 385 us a call in a stream, 206 GFLOP of the definition, at 2.05 GHz;
 // 18 products of 32x32x16 a unit of 32 candidates x 32 summaries, 12 of them the definition's, are 144 us of the matrix pipe, and
 // 32 exponentials and some 90 plain vector instructions a lane and unit nearly as much of the vector unit; the rest is what a wave
 // alone on its SIMD waits for: a tile's start and its statistics between the walks.  With a mask on every block instead of the last
-// few: 459.  Two users x 100 candidates: 15.5 us, one tile a wave, of which most is code that is walked once.
+// few: 459.  Two users x 100 candidates: 14 us, one tile a wave, of which most is code that is walked once.
 #include "grad_mfma.hpp"
 
 namespace vista {
@@ -106,19 +106,29 @@ __global__ __launch_bounds__(64, 1) void attend_grad_kernel(AttendGradParams p) 
 
   // summaries into LDS, and the square of their largest norm
   float top = 0.f;
-  #pragma unroll 4
-  for (int i = lane; i < NKB * 32 * 4; i += 64) {
-    const int row = i / 4, cn = i % 4;
-    Pack8 v;
-    v.u = u32x4{0, 0, 0, 0};
-    if (row < p.S) v.u = *reinterpret_cast<const u32x4*>(Y + int64_t(row) * p.d + 8 * cn);
-    put_row_chunk(rows, row, cn, v.u);
-    float n = 0.f;
+  // loads under way at a time, two a block of summaries; rows beyond S read the last one, since a load behind a condition waits for
+  // the one before (1024 x 512 candidates: 444 us instead of 424; 833 x 10, S = 490: 134 instead of 113)
+  constexpr int kBatch = NKB % 4 == 0 ? 8 : NKB % 2 == 0 ? 4 : 2;
+  for (int from = 0; from < 2 * NKB; from += kBatch) {
+    u32x4 raw[kBatch];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) n = fmaf(element(v, j), element(v, j), n);
-    n += __shfl_xor(n, 1, 64);           // four lanes a row
-    n += __shfl_xor(n, 2, 64);
-    top = n > top || n != n ? n : top;   // NaN stays: no tile is then bounded
+    for (int n = 0; n < kBatch; ++n) {
+      const int row = 16 * (from + n) + lane / 4, cn = lane % 4;
+      raw[n] = *reinterpret_cast<const u32x4*>(Y + int64_t(row < p.S ? row : p.S - 1) * p.d + 8 * cn);
+    }
+#pragma unroll
+    for (int n = 0; n < kBatch; ++n) {
+      const int row = 16 * (from + n) + lane / 4, cn = lane % 4;
+      Pack8 v;
+      v.u = row < p.S ? raw[n] : u32x4{0, 0, 0, 0};
+      put_row_chunk(rows, row, cn, v.u);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sum = fmaf(element(v, j), element(v, j), sum);
+      sum += __shfl_xor(sum, 1, 64);     // four lanes a row
+      sum += __shfl_xor(sum, 2, 64);
+      top = sum > top || sum != sum ? sum : top;   // NaN stays: no tile is then bounded
+    }
   }
   for (int i = lane; i < NKB * 32; i += 64) beyond[i] = i < p.S ? 0.f : -__builtin_inff();
 #pragma unroll
