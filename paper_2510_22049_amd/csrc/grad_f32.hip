@@ -16,7 +16,7 @@
 // Head widths that are no multiple of 16 are padded with zeros on their way into LDS and registers.
 //
 // Measured: one user of 1024 items, d = 64, one head, 16 queries, fp32: 32 us, five launches of 4 to 11 us, all latency.  75 users x 333
-// candidates, d = 64, one head, 100 summaries, with the self term: 41 us, 5 of them the join; 61 with a pass for the
+// candidates, d = 64, one head, 100 summaries, with the self term: 39 us, 5 of them the join; 61 with a pass for the
 // candidates' rows and one for the summaries' rows, each forming scores and dP (as beyond 128 summaries).
 #include "common.hpp"
 #include "grad.hpp"

@@ -25,7 +25,7 @@
 // independent from item to item and do not add up), and so is the output.  Measured against fp64, 2-norm: dQ, dK and dV 1.7e-3
 // to 2.4e-3, of which 1.7e-3 is the output's rounding.
 //
-// Measured, 64 users with 768597 items, d = 128, H = 4, S = 256: 707 us, of it 300 the statistics, 385 the gradients (as parts of a
+// Measured, 64 users with 768597 items, d = 128, H = 4, S = 256: 703 us, of it 300 the statistics, 385 the gradients (as parts of a
 // stream of calls; by themselves 310 and 500, at a lower clock), 15 the joins.  22 products of 32x32x16 a unit of 32 queries x 32
 // items, 10 of them the definition's, are 310 us of the matrix pipe at the 1.7 GHz that the gradients' kernel runs at; the rest
 // is what a wave alone on its SIMD cannot hide: two exponentials' worth of vector work beside a product, and a tile's start
